@@ -68,6 +68,8 @@ typedef enum ee_status {
 typedef enum ee_dtype {
   EE_F32 = 0,
   EE_BF16 = 1,
+  EE_E4M3 = 2, /* 8-bit codes of ee_scaled: 4 exponent, 3 mantissa bits, no infinity, largest 448 */
+  EE_E5M2 = 3, /* 5 exponent, 2 mantissa bits, largest finite 57344                               */
   EE_DTYPE_RANGE_MIN = -0x7FFFFFFF - 1,
   EE_DTYPE_RANGE_MAX = 0x7FFFFFFF
 } ee_dtype;
@@ -264,6 +266,116 @@ ee_status ee_exit_decide_static(const ee_exit *e, const void *hidden,
                                 int64_t n_rows, float threshold,
                                 int32_t *token, float *confidence,
                                 int32_t *exit_flag, void *stream);
+
+/* ---------------------------------------------- 8-bit block-scaled matrices
+ * A matrix of 8-bit floating-point codes with an fp32 scale for each block of
+ * 128 columns and block_rows rows: element (r, k) has the value
+ *
+ *   data[r * ld + k] * scale[(k / 128) * scale_ld + r / block_rows].
+ *
+ * A decode call streams its weights once, so 8-bit ones take half the time of
+ * bf16 ones; a training product of such matrices has twice the matrix rate. */
+typedef struct ee_scaled {
+  void *data;         /* device [rows][ld] codes; with columns cols .. the next multiple of 16 zero */
+  float *scale;       /* device [ceil(cols / 128)][scale_ld]                      */
+  int64_t rows;       /* 1 <= rows <= 1048576                                     */
+  int64_t cols;       /* 1 <= cols <= 1048576                                     */
+  int64_t ld;         /* a multiple of 16, cols <= ld <= 4194304                  */
+  int64_t scale_ld;   /* >= ceil(rows / block_rows)                               */
+  int32_t dtype;      /* EE_E4M3 or EE_E5M2                                       */
+  int32_t block_rows; /* 1 or 128                                                 */
+} ee_scaled;
+
+/* Quantises x [rows][ldx] (x_dtype: EE_F32 or EE_BF16; ldx >= cols) into q, and
+ * its transpose into qt; one of them may be NULL.  With M the largest code
+ * (448 or 57344), each block gets scale = max(max |x| / M, 2^-100) and its
+ * elements the codes nearest to x * (1 / scale), ties to even; division,
+ * reciprocal and product in fp32.  q must be rows x cols and qt cols x rows; a
+ * descriptor may count its padding columns up to the next multiple of 16.  The
+ * padding columns up to there are written as zeros; bytes and scales past that
+ * are left as they were.  NaN is left out of a block's maximum and has the code
+ * NaN; an infinity makes its block's scale infinite (products with it are NaN).
+ *
+ * Blocks of 1 row suit activations and gradients, blocks of 128 weights (whose
+ * transpose then has the same scales).  For the three products of a linear layer
+ * Y = X W^T:  Y from X and W;  dX from dY and the transpose of W;  dW from the
+ * transposes of dY and X, each with blocks of 128 tokens of one feature. */
+ee_status ee_quantize_blocks(const void *x, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ldx, const ee_scaled *q,
+                             const ee_scaled *qt, void *stream);
+
+/* C[i][j] (=|+=) sum_k A[i][k] B[j][k] for a (rows i) and b (rows j), which have the
+ * same number of columns (padding to the next multiple of 16 does not count).
+ * The dot products over a block of 128 columns are scaled and added up in fp32.
+ * For an fp32 C they are fp32 sums of exact products; for a bf16 C the 8-bit
+ * matrix instruction forms them, which cuts every product to 2^-13 of the
+ * largest of the eight it stands with (together about 1.5e-5 of the result, where
+ * C's own rounding is up to 2^-8).  a may be EE_E4M3 or EE_E5M2, b is EE_E4M3.
+ *   c        device [a->rows][ldc], c_dtype EE_F32 or EE_BF16 (rounded once), ldc
+ *            >= b->rows; columns past b->rows are left as they were.
+ *   accumulate = 0 overwrites C, 1 adds to it (EE_F32 only).
+ * Equal calls give equal results. */
+ee_status ee_scaled_matmul(const ee_scaled *a, const ee_scaled *b, void *c, int32_t c_dtype, int64_t ldc, int accumulate,
+                           void *stream);
+
+/* ---------------------------------------------------------------- logits
+ * The logits of an exit, for callers that sample, score or mix them
+ * (ee_exit_decide keeps none): logits[n][v] = (exit(hidden_n) W_out^T)[v].
+ *   w_out    NULL: the exit's own w_out.  Else an EE_E4M3 matrix V x h that takes
+ *            its place (e->w_out is ignored and may be NULL): the rows it
+ *            multiplies, in fp32 up to there, are then quantised with a scale
+ *            for each row and 128 values, as ee_quantize_blocks does.  The
+ *            rest of an MLP exit keeps the exit's dtype.
+ *   hidden   device [n_rows][h], dtype of the exit.
+ *   logits   device [n_rows][ld], logits_dtype EE_F32 or EE_BF16, ld >= V; columns
+ *            past V are left as they were.
+ *   ws       device workspace of ws_bytes >= ee_logits_workspace_bytes(). */
+size_t ee_logits_workspace_bytes(const ee_exit *e, const ee_scaled *w_out, int64_t n_rows);
+
+ee_status ee_exit_logits(const ee_exit *e, const ee_scaled *w_out, const void *hidden, int64_t n_rows, void *logits,
+                         int32_t logits_dtype, int64_t ld, void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------- sampling
+ * A token for each row of logits, from a given random number; next to it what
+ * ee_exit_decide answers, so that an exit can sample.  Per row, over the allowed
+ * tokens with logits x above -infinity, ordered by falling logit and then rising
+ * id, mass_i = exp((x_i - max x) / temperature):
+ *
+ *   top_k   > 0: the first top_k of the order;
+ *   top_p   < 1: the shortest prefix whose mass is at least top_p times the mass
+ *           of what top_k leaves (the first token at least);
+ *   min_p   > 0: those with mass_i >= min(min_p, 1)  (the largest mass is 1);
+ *   token   the lowest id whose kept mass, summed in the order of ids, exceeds
+ *           uniform times the whole kept mass (if uniform is 1 or more, the
+ *           highest id kept that has mass);
+ *   prob    its share of the kept mass;
+ *   confidence  max softmax(x) over all allowed tokens, at temperature 1;
+ *   exit_flag   confidence > threshold ? 1 : 0.
+ *
+ * temperature <= 0 takes the first of the order (prob 1).  Masses and sums are
+ * held in 64 bits.  A row whose allowed logits are all -infinity, or have a NaN
+ * or +infinity among them, or whose temperature, top_p, min_p or uniform is NaN, has no
+ * distribution: token -1, prob and confidence 0, exit_flag 0.  What stands in
+ * places that are not allowed does not matter.
+ *   logits   device [n_rows][ld], dtype EE_F32 or EE_BF16, ld >= vocab.
+ *   allowed  device [n_rows][allowed_ld] words of 32 bits, or NULL (all): bit v mod 32
+ *            of word v / 32 is 1 if token v may be taken; allowed_ld >= ceil(vocab / 32).
+ *   s        host struct of device [n_rows] arrays, each or s itself NULL for 1, 0, 1, 0.
+ *   uniform  device [n_rows] fp32 in [0, 1).
+ *   token    device [n_rows] int32;  prob, confidence (fp32) and exit_flag (int32)
+ *            device [n_rows] or NULL.
+ *   ws       device workspace of ws_bytes >= ee_sample_workspace_bytes(). */
+typedef struct ee_sampling {
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p;
+  const float *min_p;
+} ee_sampling;
+
+size_t ee_sample_workspace_bytes(int64_t n_rows, int64_t vocab);
+
+ee_status ee_sample(const void *logits, int32_t dtype, int64_t n_rows, int64_t vocab, int64_t ld, const uint32_t *allowed,
+                    int64_t allowed_ld, const ee_sampling *s, const float *uniform, float threshold, int32_t *token,
+                    float *prob, float *confidence, int32_t *exit_flag, void *ws, size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------- update
  * Adam update of exit parameters: the optimiser of Sec. 3 ("Tuning": Adam

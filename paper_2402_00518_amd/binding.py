@@ -27,6 +27,8 @@ EE_ERR_HIP = 9
 
 EE_F32 = 0
 EE_BF16 = 1
+EE_E4M3 = 2
+EE_E5M2 = 3
 
 EE_EXIT_EMBEDDING = 0
 EE_EXIT_NORM = 1
@@ -46,7 +48,8 @@ EXPORTS = (
     "ee_multi_exit_step", "ee_check_device_error", "ee_status_string",
     "ee_last_error", "ee_abi_version", "ee_profile_start", "ee_profile_stop",
     "ee_adam_update", "ee_lr_schedule", "ee_decode_workspace_bytes", "ee_exit_decide",
-    "ee_exit_decide_static",
+    "ee_exit_decide_static", "ee_quantize_blocks", "ee_scaled_matmul", "ee_logits_workspace_bytes",
+    "ee_exit_logits", "ee_sample_workspace_bytes", "ee_sample",
 )
 # Size of the fixed workspace array of ee_exit_decide_static, per GPU.
 EE_STATIC_SCRATCH_BYTES = 32 << 20
@@ -80,6 +83,18 @@ class EeAdamTensor(ctypes.Structure):
         ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
         ("numel", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32),
     ]
+
+
+class EeScaled(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+        ("ld", ctypes.c_int64), ("scale_ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("block_rows", ctypes.c_int32),
+    ]
+
+
+class EeSampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+                ("min_p", ctypes.c_void_p)]
 
 
 class EeKernelTime(ctypes.Structure):
@@ -141,6 +156,19 @@ def lib() -> ctypes.CDLL:
         L.ee_exit_decide.restype = i32
         L.ee_exit_decide_static.argtypes = [P(EeExit), vp, i64, f32, vp, vp, vp, vp]
         L.ee_exit_decide_static.restype = i32
+        sz = ctypes.c_size_t
+        L.ee_quantize_blocks.argtypes = [vp, i32, i64, i64, i64, P(EeScaled), P(EeScaled), vp]
+        L.ee_quantize_blocks.restype = i32
+        L.ee_scaled_matmul.argtypes = [P(EeScaled), P(EeScaled), vp, i32, i64, i32, vp]
+        L.ee_scaled_matmul.restype = i32
+        L.ee_logits_workspace_bytes.argtypes = [P(EeExit), P(EeScaled), i64]
+        L.ee_logits_workspace_bytes.restype = sz
+        L.ee_exit_logits.argtypes = [P(EeExit), P(EeScaled), vp, i64, vp, i32, i64, vp, sz, vp]
+        L.ee_exit_logits.restype = i32
+        L.ee_sample_workspace_bytes.argtypes = [i64, i64]
+        L.ee_sample_workspace_bytes.restype = sz
+        L.ee_sample.argtypes = [vp, i32, i64, i64, i64, vp, i64, P(EeSampling), vp, f32, vp, vp, vp, vp, vp, sz, vp]
+        L.ee_sample.restype = i32
         _lib = L
     return _lib
 
@@ -297,3 +325,69 @@ def ee_exit_decide_static(e: EeExit, hidden, n_rows: int, threshold: float, toke
     s = lib().ee_exit_decide_static(ctypes.byref(e), ptr(hidden), n_rows, threshold, ptr(token),
                                     ptr(confidence), ptr(exit_flag), stream)
     return _check(s, "ee_exit_decide_static") if check else s
+
+
+def make_scaled(data, scale, block_rows: int = 1, dtype: int = EE_E4M3, rows: Optional[int] = None,
+                cols: Optional[int] = None, ld: Optional[int] = None, scale_ld: Optional[int] = None) -> EeScaled:
+    """Descriptor of an 8-bit block-scaled matrix.  With torch tensors (codes
+    [rows][cols] of any 8-bit type, scales [column block][row block]), sizes and
+    strides default to theirs (neighbouring columns, and row blocks, adjacent)."""
+    for t in (data, scale):
+        if hasattr(t, "stride") and t.dim() == 2 and t.shape[1] > 1 and t.stride(1) != 1:
+            raise ValueError("codes and scales need stride 1 along their second dimension")
+    if rows is None:
+        rows = data.shape[0]
+    if cols is None:
+        cols = data.shape[1]
+    if ld is None:
+        ld = data.stride(0)
+    if scale_ld is None:
+        scale_ld = scale.stride(0)
+    return EeScaled(ptr(data), ptr(scale), rows, cols, ld, scale_ld, dtype, block_rows)
+
+
+def make_sampling(temperature=None, top_k=None, top_p=None, min_p=None) -> EeSampling:
+    return EeSampling(ptr(temperature), ptr(top_k), ptr(top_p), ptr(min_p))
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def ee_quantize_blocks(x, x_dtype: int, rows: int, cols: int, ldx: int, q: Optional[EeScaled], qt: Optional[EeScaled],
+                       stream, check=True) -> int:
+    s = lib().ee_quantize_blocks(ptr(x), x_dtype, rows, cols, ldx, _ref(q), _ref(qt), stream)
+    return _check(s, "ee_quantize_blocks") if check else s
+
+
+def ee_scaled_matmul(a: EeScaled, b: EeScaled, c, c_dtype: int, ldc: int, accumulate: int, stream, check=True) -> int:
+    s = lib().ee_scaled_matmul(_ref(a), _ref(b), ptr(c), c_dtype, ldc, accumulate, stream)
+    return _check(s, "ee_scaled_matmul") if check else s
+
+
+def ee_logits_workspace_bytes(e: EeExit, w_out: Optional[EeScaled], n_rows: int) -> int:
+    n = lib().ee_logits_workspace_bytes(_ref(e), _ref(w_out), n_rows)
+    if n == 0:
+        raise EEError(EE_ERR_SHAPE, "ee_logits_workspace_bytes", ee_last_error())
+    return n
+
+
+def ee_exit_logits(e: EeExit, w_out: Optional[EeScaled], hidden, n_rows: int, logits, logits_dtype: int, ld: int, ws,
+                   ws_bytes: int, stream, check=True) -> int:
+    s = lib().ee_exit_logits(_ref(e), _ref(w_out), ptr(hidden), n_rows, ptr(logits), logits_dtype, ld, ptr(ws), ws_bytes,
+                             stream)
+    return _check(s, "ee_exit_logits") if check else s
+
+
+def ee_sample_workspace_bytes(n_rows: int, vocab: int) -> int:
+    n = lib().ee_sample_workspace_bytes(n_rows, vocab)
+    if n == 0:
+        raise EEError(EE_ERR_SHAPE, "ee_sample_workspace_bytes", ee_last_error())
+    return n
+
+
+def ee_sample(logits, dtype: int, n_rows: int, vocab: int, ld: int, allowed, allowed_ld: int, sampling: Optional[EeSampling],
+              uniform, threshold: float, token, prob, confidence, exit_flag, ws, ws_bytes: int, stream, check=True) -> int:
+    s = lib().ee_sample(ptr(logits), dtype, n_rows, vocab, ld, ptr(allowed), allowed_ld, _ref(sampling), ptr(uniform),
+                        threshold, ptr(token), ptr(prob), ptr(confidence), ptr(exit_flag), ptr(ws), ws_bytes, stream)
+    return _check(s, "ee_sample") if check else s

@@ -18,7 +18,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libeetune.so")
 
 SOURCES = ["gemm_weight_grad.hip", "gemm_logits.hip", "gemm_mlp_forward.hip", "gemm_mlp_backward.hip",
-           "kernels.hip", "optim.hip", "decode.hip", "ee_abi.cpp"]
+           "kernels.hip", "optim.hip", "decode.hip", "quantize.hip", "scaled_gemm.hip", "sample.hip", "ee_abi.cpp"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

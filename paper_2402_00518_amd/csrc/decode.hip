@@ -284,6 +284,40 @@ struct DecLogits {
   }
 };
 
+// The logits themselves, out[j][ld] in fp32 or bf16; vec: groups of four of a row
+// are aligned.
+struct DecStoreLogits {
+  static constexpr bool kSplit = false;
+  struct Params {
+    void *out;
+    int64_t ld;
+    bool f32, vec;
+  };
+  __device__ __forceinline__ static void apply(const Params &p, const f32x16_t &acc, int r0, int j0, int lane, int R,
+                                               int B) {
+    for_rows4(acc, r0, j0, lane, R, B, [&](int row0, int j, f32x4_t c) EE_ALWAYS_INLINE {
+      const int64_t o = static_cast<int64_t>(j) * p.ld + row0;
+      float *f = static_cast<float *>(p.out) + o;
+      bf16_t *h = static_cast<bf16_t *>(p.out) + o;
+      if (p.vec && row0 + 4 <= R) {
+        if (p.f32)
+          dstore4<float>(f, c);
+        else
+          dstore4<bf16_t>(h, c);
+        return;
+      }
+      static_for<4>([&](auto e) EE_ALWAYS_INLINE {
+        constexpr int E = decltype(e)::value;
+        if (row0 + E >= R) return;
+        if (p.f32)
+          f[E] = c[E];
+        else
+          h[E] = f32_to_bf16(c[E]);
+      });
+    });
+  }
+};
+
 // One block of 256 threads per token: combine the tiles' partials.  Each
 // thread scans every 256th tile, then the waves combine by shuffles and the
 // four waves through LDS (two barriers per reduction).
@@ -639,6 +673,14 @@ hipError_t decode_logits(bool f32, const void *w_out, int vocab, const void *z, 
   if (f32 || decode_skinny_logits(vocab, n, h))
     EE_DISPATCH(f32, return (launch_skinny<T, DecLogits>(w_out, h, vocab, z, h, n, h, ep, stream)));
   return launch_ring<DecLogits, false>(Operand{w_out, h}, vocab, Operand{z, h}, n, h, 1, ep, stream, exact);
+}
+
+hipError_t decode_store_logits(bool f32, const void *w_out, int vocab, const void *z, int n, int h, void *out, bool out_f32,
+                               int64_t ld, hipStream_t stream) {
+  const DecStoreLogits::Params ep{out, ld, out_f32, ld % 4 == 0};
+  if (f32 || decode_skinny_logits(vocab, n, h))
+    EE_DISPATCH(f32, return (launch_skinny<T, DecStoreLogits>(w_out, h, vocab, z, h, n, h, ep, stream)));
+  return launch_ring<DecStoreLogits, false>(Operand{w_out, h}, vocab, Operand{z, h}, n, h, 1, ep, stream);
 }
 
 hipError_t decode_decide(const float *part_m, const float *part_l, const int32_t *part_arg, int tiles, int n,

@@ -161,7 +161,8 @@ ee_status check_opt_ptr(const void *p, const char *what) {
     if (_s != EE_OK) return _s;      \
   } while (0)
 
-ee_status validate_exit(const ee_exit *e, int idx) {
+// own_w: the exit's own output matrix is used (else one in 8 bits takes its place).
+ee_status validate_exit(const ee_exit *e, int idx, bool own_w = true) {
   if (e == nullptr) return fail(EE_ERR_NULL, "exit %d descriptor is NULL", idx);
   if (e->kind == EE_EXIT_LAYER)
     return fail(EE_ERR_UNSUPPORTED, "exit %d: the Layer exit (a full Transformer layer) is not implemented", idx);
@@ -192,7 +193,7 @@ ee_status validate_exit(const ee_exit *e, int idx) {
   if (e->beta != nullptr && e->norm != EE_NORM_LAYER)
     return fail(EE_ERR_SHAPE, "exit %d: beta is the bias of a LayerNorm exit", idx);
   EE_TRY(check_opt_ptr(e->beta, "beta"));
-  EE_TRY(check_ptr(e->w_out, "w_out"));
+  if (own_w) EE_TRY(check_ptr(e->w_out, "w_out"));
   if (e->kind != EE_EXIT_EMBEDDING) EE_TRY(check_ptr(e->gamma, "gamma"));
   if (e->kind == EE_EXIT_MLP) {
     EE_TRY(check_ptr(e->gamma_mlp, "gamma_mlp"));
@@ -238,11 +239,11 @@ int grad_ranges(const ee_exit &e, const ee_exit_grads &g, Range *out) {
   return k;
 }
 
-int param_ranges(const ee_exit &e, Range *out) {
+int param_ranges(const ee_exit &e, Range *out, bool own_w = true) {
   const size_t es = e.dtype == EE_BF16 ? 2 : 4;
   const size_t h = e.hidden, V = e.vocab, I = e.intermediate;
   int k = 0;
-  out[k++] = make_range(e.w_out, V * h * es, "w_out");
+  if (own_w) out[k++] = make_range(e.w_out, V * h * es, "w_out");
   if (e.kind != EE_EXIT_EMBEDDING) out[k++] = make_range(e.gamma, h * es, "gamma");
   if (e.beta != nullptr) out[k++] = make_range(e.beta, h * es, "beta");
   if (e.kind == EE_EXIT_MLP) {
@@ -605,13 +606,13 @@ ee_status static_scratch(void **out) {
   return EE_OK;
 }
 
-ee_status run_decide(const ee_exit &e, const void *x, int64_t n64, float threshold, int32_t *token,
-                     float *confidence, int32_t *exit_flag, void *ws, hipStream_t s) {
-  const DecLayout L = dec_layout(e, n64);
+// What an exit's output matrix multiplies: `z` in the exit's dtype (x itself for an
+// Embedding exit), or, with q, 8-bit codes of the rows before they are rounded.
+ee_status run_exit_rows(const ee_exit &e, const DecLayout &L, const void *x, int n, void *ws, const ee::ScaledMat *q,
+                        const void **z, hipStream_t s) {
   const bool f32 = e.dtype == EE_F32;
-  const int n = static_cast<int>(n64), h = static_cast<int>(e.hidden), V = static_cast<int>(e.vocab);
-  const int I = static_cast<int>(e.intermediate);
-  const void *z = x;
+  const int h = static_cast<int>(e.hidden), I = static_cast<int>(e.intermediate);
+  *z = x;
   if (e.kind == EE_EXIT_MLP) {
     EE_LAUNCH("decode mlp pre-norm", s,
               ee::launch_row_norm(f32, f32, x, n, h, e.rms_eps, e.gamma_mlp, nullptr, false, at(ws, L.u), s));
@@ -619,22 +620,145 @@ ee_status run_decide(const ee_exit &e, const void *x, int64_t n64, float thresho
               ee::decode_gate_up(f32, e.w_gate, e.w_up, I, at(ws, L.u), n, h, at(ws, L.hg), at(ws, L.act), s));
     EE_LAUNCH("decode down projection + residual", s,
               ee::decode_residual(f32, e.w_down, h, at(ws, L.act), n, I, x, atf(ws, L.y), L.slices, atf(ws, L.u), s));
+    if (q != nullptr) {
+      EE_LAUNCH("decode exit norm + 8-bit codes", s,
+                ee::launch_norm_quantize(true, f32, atf(ws, L.y), n, h, e.rms_eps, e.gamma, nullptr, false, *q, s,
+                                         atf(ws, L.u), L.slices - 1));
+      return EE_OK;
+    }
     EE_LAUNCH("decode exit norm", s,
               ee::launch_row_norm(true, f32, atf(ws, L.y), n, h, e.rms_eps, e.gamma, nullptr, false, at(ws, L.z), s,
                                   atf(ws, L.u), L.slices - 1));
-    z = at(ws, L.z);
+    *z = at(ws, L.z);
+  } else if (q != nullptr) {
+    const bool normed = e.kind == EE_EXIT_NORM;
+    EE_LAUNCH("decode exit norm + 8-bit codes", s,
+              ee::launch_norm_quantize(f32, f32, x, n, h, e.rms_eps, normed ? e.gamma : nullptr, normed ? e.beta : nullptr,
+                                       e.norm == EE_NORM_LAYER, *q, s));
   } else if (e.kind == EE_EXIT_NORM) {
     EE_LAUNCH("decode exit norm", s,
               ee::launch_row_norm(f32, f32, x, n, h, e.rms_eps, e.gamma, e.beta, e.norm == EE_NORM_LAYER, at(ws, L.z),
                                   s));
-    z = at(ws, L.z);
+    *z = at(ws, L.z);
   }
+  return EE_OK;
+}
+
+ee_status run_decide(const ee_exit &e, const void *x, int64_t n64, float threshold, int32_t *token,
+                     float *confidence, int32_t *exit_flag, void *ws, hipStream_t s) {
+  const DecLayout L = dec_layout(e, n64);
+  const bool f32 = e.dtype == EE_F32;
+  const int n = static_cast<int>(n64), h = static_cast<int>(e.hidden), V = static_cast<int>(e.vocab);
+  const void *z = nullptr;
+  EE_TRY(run_exit_rows(e, L, x, n, ws, nullptr, &z, s));
   int32_t *pa = reinterpret_cast<int32_t *>(at(ws, L.pa));
   EE_LAUNCH("decode logits partials", s,
             ee::decode_logits(f32, e.w_out, V, z, n, h, atf(ws, L.pm), atf(ws, L.pl), pa, s, e.kind == EE_EXIT_EMBEDDING));
   EE_LAUNCH("decode decision", s,
             ee::decode_decide(atf(ws, L.pm), atf(ws, L.pl), pa, L.tiles, n, threshold, token, confidence, exit_flag,
                               s));
+  return EE_OK;
+}
+
+// ------------------------------------------- 8-bit block-scaled matrices
+constexpr int64_t kMaxScaledLd = 1 << 22;
+
+int64_t pad16(int64_t v) { return (v + 15) / 16 * 16; }
+
+ee_status validate_scaled(const ee_scaled *m, const char *what) {
+  if (m == nullptr) return fail(EE_ERR_NULL, "%s is NULL", what);
+  if (m->dtype != EE_E4M3 && m->dtype != EE_E5M2) return fail(EE_ERR_DTYPE, "%s: dtype %d is no 8-bit type", what, m->dtype);
+  if (m->block_rows != 1 && m->block_rows != 128)
+    return fail(EE_ERR_SHAPE, "%s: block_rows = %d must be 1 or 128", what, m->block_rows);
+  if (m->rows < 1 || m->rows > kMaxTokens || m->cols < 1 || m->cols > kMaxTokens)
+    return fail(EE_ERR_SHAPE, "%s: rows = %lld and cols = %lld must be in [1, %lld]", what, static_cast<long long>(m->rows),
+                static_cast<long long>(m->cols), static_cast<long long>(kMaxTokens));
+  if (m->ld < m->cols || m->ld % 16 != 0 || m->ld > kMaxScaledLd)
+    return fail(EE_ERR_SHAPE, "%s: ld = %lld must be a multiple of 16 in [cols, %lld]", what, static_cast<long long>(m->ld),
+                static_cast<long long>(kMaxScaledLd));
+  if (m->scale_ld < cdiv64(m->rows, m->block_rows) || m->scale_ld > kMaxTokens)
+    return fail(EE_ERR_SHAPE, "%s: scale_ld = %lld must be in [ceil(rows / block_rows), %lld]", what,
+                static_cast<long long>(m->scale_ld), static_cast<long long>(kMaxTokens));
+  EE_TRY(check_ptr(m->data, what));
+  return check_ptr(m->scale, what);
+}
+
+ee::ScaledMat scaled_mat(const ee_scaled &m) {
+  return ee::ScaledMat{static_cast<uint8_t *>(m.data), m.scale, m.ld, m.scale_ld, static_cast<int>(m.rows),
+                       static_cast<int>(m.cols), m.block_rows == 128 ? 7 : 0, m.dtype == EE_E5M2};
+}
+
+// The bytes of a matrix's codes and scales (from the first to the last that is used).
+void scaled_ranges(const ee_scaled &m, Range *out) {
+  out[0] = make_range(m.data, static_cast<size_t>((m.rows - 1) * m.ld + pad16(m.cols)), "codes");
+  out[1] = make_range(m.scale, static_cast<size_t>((cdiv64(m.cols, 128) - 1) * m.scale_ld + cdiv64(m.rows, m.block_rows)) * 4,
+                      "scales");
+}
+
+// The first `n_outs` ranges must overlap neither each other nor any after them.
+ee_status check_disjoint(const Range *r, int n_outs, int n) {
+  for (int a = 0; a < n_outs; ++a)
+    for (int b = a + 1; b < n; ++b)
+      if (overlap(r[a], r[b])) return fail(EE_ERR_ALIAS, "%s overlaps %s", r[a].what, r[b].what);
+  return EE_OK;
+}
+
+size_t element_bytes(int32_t dtype) { return dtype == EE_BF16 ? 2 : 4; }
+
+// Bytes from the first to the last element of a matrix of `rows` rows.
+size_t matrix_bytes(int64_t rows, int64_t cols, int64_t ld, int32_t dtype) {
+  return static_cast<size_t>((rows - 1) * ld + cols) * element_bytes(dtype);
+}
+
+constexpr int64_t kMaxLd = int64_t{1} << 40;
+
+// ------------------------------------------------------------ exit logits
+// The decode regions, and with 8-bit weights the codes and scales of the rows.
+struct LogitsLayout {
+  DecLayout dec;
+  int64_t ldq = 0;
+  size_t codes = 0, scales = 0, total = 0;
+};
+
+LogitsLayout logits_layout(const ee_exit &e, bool scaled, int64_t n) {
+  LogitsLayout L;
+  L.dec = dec_layout(e, n);
+  L.total = e.kind == EE_EXIT_MLP ? L.dec.total : scaled ? 0 : L.dec.pm;  // (else only z is needed)
+  if (scaled) {
+    L.ldq = e.hidden;  // a multiple of 64
+    L.codes = L.total;
+    L.scales = align_up(L.codes + static_cast<size_t>(n * L.ldq));
+    L.total = align_up(L.scales + static_cast<size_t>(cdiv64(e.hidden, 128) * n) * 4);
+  }
+  return L;
+}
+
+ee_status validate_logits_exit(const ee_exit *e, const ee_scaled *w, int64_t n_rows) {
+  EE_TRY(validate_exit(e, 0, w == nullptr));
+  EE_TRY(validate_rows(n_rows));
+  if (w == nullptr) return EE_OK;
+  EE_TRY(validate_scaled(w, "w_out"));
+  if (w->dtype != EE_E4M3) return fail(EE_ERR_DTYPE, "w_out must be EE_E4M3");
+  if (w->rows != e->vocab || w->cols != e->hidden)
+    return fail(EE_ERR_SHAPE, "w_out is %lld x %lld, the exit's is %lld x %lld", static_cast<long long>(w->rows),
+                static_cast<long long>(w->cols), static_cast<long long>(e->vocab), static_cast<long long>(e->hidden));
+  return EE_OK;
+}
+
+ee_status run_logits(const ee_exit &e, const ee_scaled *w, const void *x, int64_t n64, void *logits, int32_t dtype, int64_t ld,
+                     void *ws, hipStream_t s) {
+  const LogitsLayout L = logits_layout(e, w != nullptr, n64);
+  const bool out_f32 = dtype == EE_F32;
+  const int n = static_cast<int>(n64), h = static_cast<int>(e.hidden), V = static_cast<int>(e.vocab);
+  const void *z = nullptr;
+  if (w != nullptr) {
+    const ee::ScaledMat q{reinterpret_cast<uint8_t *>(at(ws, L.codes)), atf(ws, L.scales), L.ldq, n64, n, h, 0, false};
+    EE_TRY(run_exit_rows(e, L.dec, x, n, ws, &q, &z, s));
+    EE_LAUNCH("decode 8-bit logits", s, ee::scaled_matmul(q, scaled_mat(*w), logits, out_f32, ld, 0, s));
+    return EE_OK;
+  }
+  EE_TRY(run_exit_rows(e, L.dec, x, n, ws, nullptr, &z, s));
+  EE_LAUNCH("decode logits", s, ee::decode_store_logits(e.dtype == EE_F32, e.w_out, V, z, n, h, logits, out_f32, ld, s));
   return EE_OK;
 }
 
@@ -880,6 +1004,155 @@ ee_status ee_exit_decide_static(const ee_exit *e, const void *hidden, int64_t n_
                                   static_cast<hipStream_t>(stream));
   g_prof_suspended = was;
   return st;
+}
+
+ee_status ee_quantize_blocks(const void *x, int32_t x_dtype, int64_t rows, int64_t cols, int64_t ldx, const ee_scaled *q,
+                             const ee_scaled *qt, void *stream) {
+  g_last_error.clear();
+  if (x_dtype != EE_F32 && x_dtype != EE_BF16) return fail(EE_ERR_DTYPE, "x_dtype %d is neither EE_F32 nor EE_BF16", x_dtype);
+  if (rows < 1 || rows > kMaxTokens || cols < 1 || cols > kMaxTokens)
+    return fail(EE_ERR_SHAPE, "rows = %lld and cols = %lld must be in [1, %lld]", static_cast<long long>(rows),
+                static_cast<long long>(cols), static_cast<long long>(kMaxTokens));
+  if (ldx < cols || ldx > kMaxLd) return fail(EE_ERR_SHAPE, "ldx = %lld is less than cols, or too large", static_cast<long long>(ldx));
+  EE_TRY(check_ptr(x, "x"));
+  if (q == nullptr && qt == nullptr) return fail(EE_ERR_NULL, "q and qt are both NULL");
+  Range r[5];
+  int k = 0;
+  ee::ScaledMat a{}, b{};
+  if (q != nullptr) {
+    EE_TRY(validate_scaled(q, "q"));
+    if (q->rows != rows || q->cols < cols || q->cols > pad16(cols))
+      return fail(EE_ERR_SHAPE, "q is %lld x %lld, x is %lld x %lld", static_cast<long long>(q->rows),
+                  static_cast<long long>(q->cols), static_cast<long long>(rows), static_cast<long long>(cols));
+    scaled_ranges(*q, r + k);
+    k += 2;
+    a = scaled_mat(*q);
+  }
+  if (qt != nullptr) {
+    EE_TRY(validate_scaled(qt, "qt"));
+    if (qt->rows != cols || qt->cols < rows || qt->cols > pad16(rows))
+      return fail(EE_ERR_SHAPE, "qt is %lld x %lld, x is %lld x %lld", static_cast<long long>(qt->rows),
+                  static_cast<long long>(qt->cols), static_cast<long long>(rows), static_cast<long long>(cols));
+    scaled_ranges(*qt, r + k);
+    k += 2;
+    b = scaled_mat(*qt);
+  }
+  r[k] = make_range(x, matrix_bytes(rows, cols, ldx, x_dtype), "x");
+  EE_TRY(check_disjoint(r, k, k + 1));
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  EE_LAUNCH("8-bit codes", s,
+            ee::launch_quantize(x_dtype == EE_F32, x, ldx, static_cast<int>(rows), static_cast<int>(cols),
+                                q != nullptr ? &a : nullptr, qt != nullptr ? &b : nullptr, s));
+  return EE_OK;
+}
+
+ee_status ee_scaled_matmul(const ee_scaled *a, const ee_scaled *b, void *c, int32_t c_dtype, int64_t ldc, int accumulate,
+                           void *stream) {
+  g_last_error.clear();
+  EE_TRY(validate_scaled(a, "a"));
+  EE_TRY(validate_scaled(b, "b"));
+  if (b->dtype != EE_E4M3) return fail(EE_ERR_DTYPE, "b must be EE_E4M3");
+  if (pad16(a->cols) != pad16(b->cols))
+    return fail(EE_ERR_SHAPE, "a has %lld columns, b %lld", static_cast<long long>(a->cols), static_cast<long long>(b->cols));
+  if (c_dtype != EE_F32 && c_dtype != EE_BF16) return fail(EE_ERR_DTYPE, "c_dtype %d is neither EE_F32 nor EE_BF16", c_dtype);
+  if (accumulate != 0 && accumulate != 1) return fail(EE_ERR_SHAPE, "accumulate must be 0 or 1");
+  if (accumulate != 0 && c_dtype != EE_F32) return fail(EE_ERR_UNSUPPORTED, "accumulate needs c_dtype EE_F32");
+  if (ldc < b->rows || ldc > kMaxLd) return fail(EE_ERR_SHAPE, "ldc = %lld is less than b's rows, or too large", static_cast<long long>(ldc));
+  EE_TRY(check_ptr(c, "c"));
+  Range r[5] = {make_range(c, matrix_bytes(a->rows, b->rows, ldc, c_dtype), "c")};
+  scaled_ranges(*a, r + 1);
+  scaled_ranges(*b, r + 3);
+  EE_TRY(check_disjoint(r, 1, 5));
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  EE_LAUNCH("8-bit product", s, ee::scaled_matmul(scaled_mat(*a), scaled_mat(*b), c, c_dtype == EE_F32, ldc, accumulate, s));
+  return EE_OK;
+}
+
+size_t ee_logits_workspace_bytes(const ee_exit *e, const ee_scaled *w_out, int64_t n_rows) {
+  g_last_error.clear();
+  if (validate_logits_exit(e, w_out, n_rows) != EE_OK) return 0;
+  return std::max(logits_layout(*e, w_out != nullptr, n_rows).total, kAlign);
+}
+
+ee_status ee_exit_logits(const ee_exit *e, const ee_scaled *w_out, const void *hidden, int64_t n_rows, void *logits,
+                         int32_t logits_dtype, int64_t ld, void *ws, size_t ws_bytes, void *stream) {
+  g_last_error.clear();
+  EE_TRY(validate_logits_exit(e, w_out, n_rows));
+  if (logits_dtype != EE_F32 && logits_dtype != EE_BF16)
+    return fail(EE_ERR_DTYPE, "logits_dtype %d is neither EE_F32 nor EE_BF16", logits_dtype);
+  if (ld < e->vocab || ld > kMaxLd) return fail(EE_ERR_SHAPE, "ld = %lld is less than the vocabulary, or too large", static_cast<long long>(ld));
+  EE_TRY(check_ptr(hidden, "hidden"));
+  EE_TRY(check_ptr(logits, "logits"));
+  const size_t need = std::max(logits_layout(*e, w_out != nullptr, n_rows).total, kAlign);
+  EE_TRY(check_workspace(ws, ws_bytes, need));
+  Range r[12] = {make_range(logits, matrix_bytes(n_rows, e->vocab, ld, logits_dtype), "logits"),
+                 make_range(ws, ws_bytes, "workspace")};
+  int k = 2 + param_ranges(*e, r + 2, w_out == nullptr);
+  r[k++] = make_range(hidden, static_cast<size_t>(n_rows * e->hidden) * element_bytes(e->dtype), "hidden");
+  if (w_out != nullptr) {
+    scaled_ranges(*w_out, r + k);
+    k += 2;
+  }
+  EE_TRY(check_disjoint(r, 2, k));
+  return run_logits(*e, w_out, hidden, n_rows, logits, logits_dtype, ld, ws, static_cast<hipStream_t>(stream));
+}
+
+size_t ee_sample_workspace_bytes(int64_t n_rows, int64_t vocab) {
+  g_last_error.clear();
+  if (validate_rows(n_rows) != EE_OK) return 0;
+  if (vocab < 1 || vocab > kMaxVocab) {
+    fail(EE_ERR_SHAPE, "vocab = %lld must be in [1, %lld]", static_cast<long long>(vocab), static_cast<long long>(kMaxVocab));
+    return 0;
+  }
+  return ee::sample_workspace(static_cast<int>(n_rows), static_cast<int>(vocab));
+}
+
+ee_status ee_sample(const void *logits, int32_t dtype, int64_t n_rows, int64_t vocab, int64_t ld, const uint32_t *allowed,
+                    int64_t allowed_ld, const ee_sampling *sp, const float *uniform, float threshold, int32_t *token,
+                    float *prob, float *confidence, int32_t *exit_flag, void *ws, size_t ws_bytes, void *stream) {
+  const size_t need = ee_sample_workspace_bytes(n_rows, vocab);
+  if (need == 0) return EE_ERR_SHAPE;
+  if (dtype != EE_F32 && dtype != EE_BF16) return fail(EE_ERR_DTYPE, "dtype %d is neither EE_F32 nor EE_BF16", dtype);
+  if (ld < vocab || ld > kMaxLd) return fail(EE_ERR_SHAPE, "ld = %lld is less than the vocabulary, or too large", static_cast<long long>(ld));
+  if (allowed != nullptr && (allowed_ld < cdiv64(vocab, 32) || allowed_ld > kMaxLd))
+    return fail(EE_ERR_SHAPE, "allowed_ld = %lld words are too few for %lld tokens, or too many", static_cast<long long>(allowed_ld),
+                static_cast<long long>(vocab));
+  if (std::isnan(threshold)) return fail(EE_ERR_SHAPE, "threshold is NaN");
+  const ee_sampling how = sp != nullptr ? *sp : ee_sampling{};
+  EE_TRY(check_ptr(logits, "logits"));
+  EE_TRY(check_opt_ptr(allowed, "allowed"));
+  EE_TRY(check_opt_ptr(how.temperature, "temperature"));
+  EE_TRY(check_opt_ptr(how.top_k, "top_k"));
+  EE_TRY(check_opt_ptr(how.top_p, "top_p"));
+  EE_TRY(check_opt_ptr(how.min_p, "min_p"));
+  EE_TRY(check_ptr(uniform, "uniform"));
+  EE_TRY(check_ptr(token, "token"));
+  EE_TRY(check_opt_ptr(prob, "prob"));
+  EE_TRY(check_opt_ptr(confidence, "confidence"));
+  EE_TRY(check_opt_ptr(exit_flag, "exit_flag"));
+  EE_TRY(check_workspace(ws, ws_bytes, need));
+  const size_t n4 = static_cast<size_t>(n_rows) * 4;
+  Range r[12];
+  int k = 0;
+  r[k++] = make_range(token, n4, "token");
+  if (prob != nullptr) r[k++] = make_range(prob, n4, "prob");
+  if (confidence != nullptr) r[k++] = make_range(confidence, n4, "confidence");
+  if (exit_flag != nullptr) r[k++] = make_range(exit_flag, n4, "exit_flag");
+  r[k++] = make_range(ws, ws_bytes, "workspace");
+  const int outs = k;
+  r[k++] = make_range(logits, matrix_bytes(n_rows, vocab, ld, dtype), "logits");
+  if (allowed != nullptr) r[k++] = make_range(allowed, static_cast<size_t>((n_rows - 1) * allowed_ld + cdiv64(vocab, 32)) * 4, "allowed");
+  if (how.temperature != nullptr) r[k++] = make_range(how.temperature, n4, "temperature");
+  if (how.top_k != nullptr) r[k++] = make_range(how.top_k, n4, "top_k");
+  if (how.top_p != nullptr) r[k++] = make_range(how.top_p, n4, "top_p");
+  if (how.min_p != nullptr) r[k++] = make_range(how.min_p, n4, "min_p");
+  r[k++] = make_range(uniform, n4, "uniform");
+  EE_TRY(check_disjoint(r, outs, k));
+  const ee::SampleArgs a{logits, ld, allowed, allowed_ld, how.temperature, how.top_k, how.top_p, how.min_p, uniform, threshold,
+                         token, prob, confidence, exit_flag, static_cast<int>(n_rows), static_cast<int>(vocab)};
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  EE_LAUNCH("sample", s, ee::launch_sample(dtype == EE_F32, a, ws, s));
+  return EE_OK;
 }
 
 ee_status ee_profile_start(void) {

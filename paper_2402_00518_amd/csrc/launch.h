@@ -264,10 +264,57 @@ hipError_t decode_residual(bool f32, const void *w, int rows, const void *z, int
 // them), so the fp32 sums are all of the error and are kept short.
 hipError_t decode_logits(bool f32, const void *w_out, int vocab, const void *z, int n, int h, float *part_m,
                          float *part_l, int32_t *part_arg, hipStream_t stream, bool exact);
+// The logits themselves: out[n][ld] in fp32 or bf16.
+hipError_t decode_store_logits(bool f32, const void *w_out, int vocab, const void *z, int n, int h, void *out, bool out_f32,
+                               int64_t ld, hipStream_t stream);
 // Greedy token, its probability, and confidence > threshold, per token row.
 hipError_t decode_decide(const float *part_m, const float *part_l, const int32_t *part_arg, int tiles, int n,
                          float threshold, int32_t *token, float *confidence, int32_t *exit_flag,
                          hipStream_t stream);
+
+// ------------------------------------------------- 8-bit block-scaled matrices
+// Codes [rows][ld] and scales [column block of 128][scale_ld], one scale for each
+// 2^shift rows (shift 0 or 7).  data NULL: no matrix.
+struct ScaledMat {
+  uint8_t *data;
+  float *scale;
+  int64_t ld, scale_ld;
+  int rows, cols;
+  int shift;
+  bool e5m2;
+};
+// x [rows][ldx] as codes (q), and transposed (qt); either may be NULL.
+hipError_t launch_quantize(bool f32, const void *x, int64_t ldx, int rows, int cols, const ScaledMat *q, const ScaledMat *qt,
+                           hipStream_t stream);
+// The rows of an exit's norm (arguments as launch_row_norm; gain NULL: the rows as
+// they are) as e4m3 codes with a scale for each row and 128 values.  h: a multiple of 64.
+hipError_t launch_norm_quantize(bool x_f32, bool f32, const void *x, int n, int h, float eps, const void *gain, const void *bias,
+                                bool centre, const ScaledMat &q, hipStream_t stream, const float *extra = nullptr, int n_extra = 0);
+// C[i][j] (=|+=) sum over column blocks of the scales' product times the codes' dot
+// product: rows of a by rows of b, C [a.rows][ldc] in fp32 or bf16.
+hipError_t scaled_matmul(const ScaledMat &a, const ScaledMat &b, void *c, bool c_f32, int64_t ldc, int accumulate,
+                         hipStream_t stream);
+
+// ---------------------------------------------------------------- sampling
+struct SampleArgs {
+  const void *logits;
+  int64_t ld;
+  const uint32_t *allowed;   // or NULL
+  int64_t allowed_ld;
+  const float *temperature;  // each or NULL
+  const int32_t *top_k;
+  const float *top_p;
+  const float *min_p;
+  const float *uniform;
+  float threshold;
+  int32_t *token;
+  float *prob;               // these three or NULL
+  float *confidence;
+  int32_t *exit_flag;
+  int n, vocab;
+};
+size_t sample_workspace(int n, int vocab);
+hipError_t launch_sample(bool f32, const SampleArgs &a, void *ws, hipStream_t stream);
 
 // Blocks one tensor of `numel` elements occupies in a launch.
 int64_t adam_blocks(int64_t numel);
