@@ -30,30 +30,48 @@ namespace ee {
 
 namespace {
 
-constexpr int kWaves = 16, kThreads = kWaves * 64;
 constexpr int kBins = 2048;
 constexpr float kBinsPerUnit = 64.0f;
-constexpr int kList = 4096;
-constexpr double kUnit = 0x1p43;  // masses in the histogram: at most 2^20 tokens of mass 1
+constexpr int kSmallList = 128;  // one wave does the rest of a row with so few tokens listed
+constexpr int kSorted = 2 * kBins;
+constexpr double kUnit = 0x1p43; // masses in the histogram: at most 2^20 tokens of mass 1
 
-// 2^t for t <= 0, relative error 1e-14: 2^f = sum (f ln 2)^k / k! on |f| <= 1/2.
-__device__ __forceinline__ double pow2_neg(double t) {
-  const double n = __builtin_rint(t), y = (t - n) * 0.69314718055994530942;
-  double p = 1.0 / 479001600.0;
-  p = __builtin_fma(p, y, 1.0 / 39916800.0);
-  p = __builtin_fma(p, y, 1.0 / 3628800.0);
-  p = __builtin_fma(p, y, 1.0 / 362880.0);
-  p = __builtin_fma(p, y, 1.0 / 40320.0);
-  p = __builtin_fma(p, y, 1.0 / 5040.0);
-  p = __builtin_fma(p, y, 1.0 / 720.0);
-  p = __builtin_fma(p, y, 1.0 / 120.0);
-  p = __builtin_fma(p, y, 1.0 / 24.0);
-  p = __builtin_fma(p, y, 1.0 / 6.0);
-  p = __builtin_fma(p, y, 0.5);
-  p = __builtin_fma(p, y, 1.0);
-  p = __builtin_fma(p, y, 1.0);
-  // (the clamp leaves 0 for -infinity and for what ldexp would underflow to)
-  return t < -1022.0 ? 0.0 : __builtin_amdgcn_ldexp(p, static_cast<int>(n));
+// e^y by its series, for the compiler.
+constexpr double series_exp(double y) {
+  double sum = 1.0, term = 1.0;
+  for (int k = 1; k < 24; ++k) {
+    term *= y / k;
+    sum += term;
+  }
+  return sum;
+}
+constexpr double kLn2 = 0.69314718055994530942;
+struct Pow2Table {
+  double v[64];  // 2^(i / 64)
+  constexpr Pow2Table() : v() {
+    for (int i = 0; i < 64; ++i) v[i] = series_exp(kLn2 * i / 64);
+  }
+};
+__device__ constexpr Pow2Table kPow2{};
+
+// 2^(t / 64) for t <= 0, relative error 4e-14: t = k + r with k whole and |r| <= 1/2, so it is
+// 2^(k div 64) table[k mod 64] e^(r ln 2 / 64), the last by its series up to the fourth power.
+// 0 below 2^-1000 (without CLEAN: 2^-1000 there, for sums in which that does not matter).
+// A sum over a vocabulary is these exponentials, so rounding and scaling are integer
+// operations on a sum with 1.5 2^52 (with the conversion and ldexp instructions, and a series
+// of twelve terms in place of the table, 32000 tokens took 13 us in one block, so 6).
+template <bool CLEAN = true>
+__device__ __forceinline__ double pow2_neg(double t, const double *table) {
+  constexpr double c1 = kLn2 / 64, c2 = c1 * c1 / 2, c3 = c1 * c2 / 3, c4 = c1 * c3 / 4;
+  const double c = fmax(t, -64000.0), shifted = c + 0x1.8p52, r = c - (shifted - 0x1.8p52);
+  const int k = static_cast<int>(static_cast<uint32_t>(__builtin_bit_cast(uint64_t, shifted)));
+  const double p = __builtin_fma(__builtin_fma(__builtin_fma(__builtin_fma(c4, r, c3), r, c2), r, c1), r, 1.0);
+  const uint64_t b = __builtin_bit_cast(uint64_t, p * table[k & 63]);
+  const double v = __builtin_bit_cast(double, b + (static_cast<uint64_t>(static_cast<uint32_t>((k >> 6) << 20)) << 32));
+  return CLEAN && !(t >= -64000.0) ? 0.0 : v;
+}
+__device__ __forceinline__ unsigned long long units_of(double mass) {  // of a mass <= 1
+  return __builtin_bit_cast(uint64_t, __builtin_fma(mass, kUnit, 0x1p52)) & 0xFFFFFFFFFFFFFull;
 }
 
 // Bits that order as the values do; -0 counts as 0.
@@ -65,127 +83,191 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
 }
 
-template <typename V>
-__device__ __forceinline__ V wave_scan(V v, int lane) {  // inclusive
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const V t = __shfl_up(v, o);
-    if (lane >= o) v += t;
+// One step of a prefix sum: the value that a DPP pattern brings to each lane, 0 where
+// it brings none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROWS, 0xF, false));
+}
+template <int CTRL, int ROWS, typename V>
+__device__ __forceinline__ V dpp_value(V v) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, dpp<CTRL, ROWS>(__builtin_bit_cast(uint32_t, v)));
+  } else {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t lo = dpp<CTRL, ROWS>(static_cast<uint32_t>(b)), hi = dpp<CTRL, ROWS>(static_cast<uint32_t>(b >> 32));
+    return __builtin_bit_cast(V, lo | hi << 32);
   }
+}
+// Inclusive prefix over the wave: within rows of 16 lanes, then the last lane of row 0
+// (and 2) to row 1 (3), and of the first two rows to the others.
+template <typename V>
+__device__ __forceinline__ V wave_scan(V v) {
+  v += dpp_value<0x111, 0xF>(v);
+  v += dpp_value<0x112, 0xF>(v);
+  v += dpp_value<0x114, 0xF>(v);
+  v += dpp_value<0x118, 0xF>(v);
+  v += dpp_value<0x142, 0xA>(v);
+  v += dpp_value<0x143, 0xC>(v);
   return v;
+}
+template <typename V>
+__device__ __forceinline__ V of_lane(V v, int lane) {  // lane: the same in all
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+  } else {
+    const uint64_t b = __builtin_bit_cast(uint64_t, v);
+    const uint64_t lo = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(b), lane)),
+                   hi = static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(b >> 32), lane));
+    return __builtin_bit_cast(V, lo | hi << 32);
+  }
 }
 template <typename V>
 __device__ __forceinline__ V wave_sum(V v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+  return of_lane(wave_scan(v), 63);
 }
 
+// LIST: tokens that the list holds, a multiple of 64 for each wave.
+template <int LIST>
 struct Shared {
   union {
     unsigned long long hist[kBins];
-    uint32_t sorted[kList];
+    uint32_t sorted[kSorted];
   };
-  uint32_t key[kList];
-  int32_t id[kList];
-  double part[2][kWaves];
-  int ipart[2][kWaves];
-  unsigned long long upart[kWaves];
-  int found;
+  uint32_t key[LIST];
+  int32_t id[LIST];
+  double table[64];
+  double part[2][16];
+  int ipart[2][16];
+  unsigned long long upart[16];
+  int found, n_sub;
   unsigned long long before;
-  int token;
-  double mass;
 };
 
-template <typename T, int IT>
+// Beside a row in LDS the list is short; without one it is as long as two blocks a CU allow.
+constexpr int list_of(bool cached) { return cached ? 2048 : 6144; }
+constexpr size_t shared_bytes(bool cached) { return ((cached ? sizeof(Shared<list_of(true)>) : sizeof(Shared<list_of(false)>)) + 15) / 16 * 16; }
+
+template <typename T> struct Quad;
+template <> struct Quad<float> { using type = f32x4_t; };
+template <> struct Quad<bf16_t> { using type = u32x2_t; };
+
+// The logits of a row, four ids a lane and step.  CACHED: in LDS (tokens that are not
+// allowed as -infinity), else read from memory again by every pass, four steps'
+// loads at once (with one, a pass over 128000 tokens waited on memory for 31 of them
+// in turn).
+template <typename T, bool CACHED>
 struct Row {
-  static constexpr int KEEP = IT > 0 ? IT : 1;
+  using Q = typename Quad<T>::type;
   const T *p;
   const uint32_t *allowed;
+  Q *cache;
   int vocab, first, last;  // ids of the wave: [first, last)
   bool vec;
   int lane;
-  float kept[KEEP][4];
+  mutable bool stop = false;  // set by a pass's function: no further step
 
-  __device__ __forceinline__ void load4(int id, float (&x)[4]) const {
-    if (vec && id + 4 <= vocab) {
-      if constexpr (std::is_same<T, float>::value) {
-        const f32x4_t v = *reinterpret_cast<const f32x4_t *>(p + id);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = v[e];
-      } else {
-        const u32x2_t v = *reinterpret_cast<const u32x2_t *>(p + id);
-        x[0] = __uint_as_float(v[0] << 16);
-        x[1] = __uint_as_float(v[0] & 0xFFFF0000u);
-        x[2] = __uint_as_float(v[1] << 16);
-        x[3] = __uint_as_float(v[1] & 0xFFFF0000u);
-      }
+  __device__ __forceinline__ static void unpack(const Q &v, float (&x)[4]) {
+    if constexpr (std::is_same<T, float>::value) {
+      static_for<4>([&](auto e) EE_ALWAYS_INLINE { x[decltype(e)::value] = v[decltype(e)::value]; });
     } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = id + e < vocab ? to_f32(p[id + e]) : -INFINITY;
-    }
-    if (allowed != nullptr && id < vocab) {
-      const uint32_t w = allowed[id >> 5] >> (id & 31);  // id is a multiple of 4
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (((w >> e) & 1) == 0) x[e] = -INFINITY;
+      x[0] = __uint_as_float(v[0] << 16);
+      x[1] = __uint_as_float(v[0] & 0xFFFF0000u);
+      x[2] = __uint_as_float(v[1] << 16);
+      x[3] = __uint_as_float(v[1] & 0xFFFF0000u);
     }
   }
-  __device__ __forceinline__ void init() {
-    if constexpr (IT > 0) {
+  __device__ __forceinline__ static Q pack(const float (&x)[4]) {
+    if constexpr (std::is_same<T, float>::value)
+      return Q{x[0], x[1], x[2], x[3]};
+    else  // (values that are bf16 already)
+      return Q{(__float_as_uint(x[0]) >> 16) | (__float_as_uint(x[1]) & 0xFFFF0000u),
+               (__float_as_uint(x[2]) >> 16) | (__float_as_uint(x[3]) & 0xFFFF0000u)};
+  }
+  // Four ids from `id` < vocab on; past the vocabulary anything.
+  __device__ __forceinline__ Q load(int id) const {
+    if (vec && id + 4 <= vocab) return *reinterpret_cast<const Q *>(p + id);
+    float x[4];
 #pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        const int id = first + i * 256 + lane * 4;
-        if (id < last)
-          load4(id, kept[i]);
-        else
-          kept[i][0] = kept[i][1] = kept[i][2] = kept[i][3] = -INFINITY;
-      }
-    }
+    for (int e = 0; e < 4; ++e) x[e] = to_f32(p[min(id + e, vocab - 1)]);
+    return pack(x);
+  }
+  // -infinity for what is not allowed (bit e of w 0) or past the vocabulary.
+  __device__ __forceinline__ void mask(int id, uint32_t w, float (&x)[4]) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (((w >> e) & 1) == 0 || id + e >= vocab) x[e] = -INFINITY;
   }
   // f(first id, values) for every four ids of this lane, in the order of ids.  Every
-  // lane of the wave takes part (ids past the last have -infinity).
-  template <class F>
+  // lane of the wave takes part (ids past the last have -infinity).  FILL: the first pass.
+  template <bool FILL = false, class F>
   __device__ __forceinline__ void each(F &&f) const {
-    if constexpr (IT > 0) {
-#pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        f(first + i * 256 + lane * 4, kept[i]);
-        __builtin_amdgcn_sched_barrier(0);  // (one group's work at a time: mixed, they need more registers than there are)
+    if constexpr (CACHED && !FILL) {
+      for (int i = first; i < last && !stop; i += 256) {
+        const int id = i + lane * 4;
+        float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if (id < last) unpack(cache[id >> 2], x);
+        f(id, x);
       }
     } else {
-      for (int i = first; i < last; i += 256) {
-        float x[4];
-        const int id = i + lane * 4;
-        if (id < last)
-          load4(id, x);
-        else
-          x[0] = x[1] = x[2] = x[3] = -INFINITY;
-        f(id, x);
+      constexpr int U = 4;
+      for (int i = first; i < last && !stop; i += 256 * U) {
+        Q raw[U];
+        uint32_t ok[U];
+#pragma unroll
+        for (int b = 0; b < U; ++b) {
+          const int id = i + b * 256 + lane * 4;
+          ok[b] = 0;
+          if (id < last) {
+            raw[b] = load(id);
+            ok[b] = allowed != nullptr ? allowed[id >> 5] >> (id & 31) : 15u;  // (id is a multiple of 4)
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < U; ++b) {
+          const int id = i + b * 256 + lane * 4;
+          if (i + b * 256 < last && !stop) {
+            float x[4];
+            unpack(raw[b], x);
+            mask(id, ok[b], x);
+            if (CACHED && id < last) cache[id >> 2] = pack(x);
+            f(id, x);
+          }
+          __builtin_amdgcn_sched_barrier(0);  // (one group at a time: mixed, they need more registers than there are)
+        }
       }
     }
   }
 };
 
-template <typename T, int IT>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
-  __shared__ Shared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = blockIdx.x;
+// W: waves of the block.
+template <typename T, bool CACHED, int W>
+__global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
+  constexpr int kThreads = 64 * W, kList = list_of(CACHED);
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  auto &sh = *reinterpret_cast<Shared<kList> *>(smem);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.x;
   const float temp = a.temperature != nullptr ? a.temperature[n] : 1.0f;
   const int top_k = a.top_k != nullptr ? a.top_k[n] : 0;
   const float top_p = a.top_p != nullptr ? a.top_p[n] : 1.0f;
   const float min_p = a.min_p != nullptr ? a.min_p[n] : 0.0f;
   const float u = a.uniform[n];
-  Row<T, IT> row;
+  Row<T, CACHED> row;
+  row.cache = reinterpret_cast<typename Quad<T>::type *>(smem + shared_bytes(CACHED));
   row.p = static_cast<const T *>(a.logits) + n * a.ld;
   row.allowed = a.allowed != nullptr ? a.allowed + n * a.allowed_ld : nullptr;
   row.vocab = a.vocab;
-  const int chunk = (a.vocab + kWaves * 256 - 1) / (kWaves * 256) * 256;
-  row.first = min(wave * chunk, a.vocab);
-  row.last = min(row.first + chunk, a.vocab);
-  row.vec = a.ld * sizeof(T) % (4 * sizeof(T)) == 0;
+  // the waves' shares of ids [from, to), whole steps of 256 ids each
+  auto share = [&](int from, int to) EE_ALWAYS_INLINE {
+    const int chunk = (to - from + W * 256 - 1) / (W * 256) * 256;
+    row.first = min(from + wave * chunk, to);
+    row.last = min(row.first + chunk, to);
+    return chunk;
+  };
+  const int chunk = share(0, a.vocab);
+  row.vec = a.ld % 4 == 0;
   row.lane = lane;
-  row.init();
 
   int slot = 0;  // block sums alternate between two slots, one barrier each
   auto block_sum = [&](double v) EE_ALWAYS_INLINE {
@@ -194,7 +276,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     __syncthreads();
     double s = 0.0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) s += sh.part[slot][w];
+    for (int w = 0; w < W; ++w) s += sh.part[slot][w];
     slot ^= 1;
     return s;
   };
@@ -202,7 +284,9 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   // 1. the maximum, and whether the row has a distribution at all
   float mx = -INFINITY;
   bool bad = temp != temp || top_p != top_p || min_p != min_p || u != u;
-  row.each([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
+  for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;  // (closed by the barrier below, as is the table)
+  if (tid < 64) sh.table[tid] = kPow2.v[tid];
+  row.template each<true>([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       mx = fmaxf(mx, x[e]);
@@ -219,7 +303,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   bad = false;
   mx = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < W; ++w) {
     mx = fmaxf(mx, static_cast<float>(sh.part[0][w]));
     bad |= sh.ipart[0][w] != 0;
   }
@@ -235,12 +319,14 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   }
   const bool greedy = !(temp > 0.0f);
   // (an infinite temperature still sends -infinity to mass 0)
-  const double dmx = mx, c1 = 1.44269504088896340736, ct = greedy ? c1 : fmax(c1 / static_cast<double>(temp), 1e-300);
-  auto mass_of = [&](float x) EE_ALWAYS_INLINE { return pow2_neg((static_cast<double>(x) - dmx) * ct); };
+  const double dmx = mx, c1 = 64.0 / kLn2, ct = greedy ? c1 : fmax(c1 / static_cast<double>(temp), 1e-300);
+  auto mass_of = [&](float x) EE_ALWAYS_INLINE { return pow2_neg((static_cast<double>(x) - dmx) * ct, sh.table); };
   const bool want_conf = a.confidence != nullptr || a.exit_flag != nullptr;
   const bool by_count = !greedy && top_k > 0 && top_k < a.vocab, by_mass = !greedy && top_p < 1.0f;
   const bool cut = by_count || by_mass;
   const bool same = ct == c1;  // one mass serves both
+  const double least = min_p > 0.0f ? (min_p < 1.0f ? static_cast<double>(min_p) : 1.0) : 0.0;
+  const double p = top_p > 0.0f ? static_cast<double>(top_p) : 0.0;
 
   // 2. sums of masses; the histogram
   const float bscale = static_cast<float>(kBinsPerUnit / (greedy ? 1.0 : static_cast<double>(temp)));
@@ -248,31 +334,33 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     const float b = (mx - x) * bscale;
     return b < static_cast<float>(kBins - 1) ? static_cast<int>(b) : kBins - 1;
   };
-  if (cut) {
-    for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;
-    __syncthreads();
-  }
   double z = 0.0, z1 = 0.0;
-  const bool need_z = (by_mass && !by_count) || (want_conf && same);
-  if (need_z || cut || want_conf) {
-    row.each([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
+  const bool need_z = (by_mass && !by_count) || (want_conf && same) || (!cut && !greedy && least == 0.0);
+  const bool need_z1 = want_conf && !same;
+  if (need_z || need_z1 || cut) {
+    auto pass = [&](auto with_z, auto with_z1, auto with_hist) EE_ALWAYS_INLINE {
+      row.each([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        double m = 0.0;
-        if (need_z) {
-          m = mass_of(x[e]);
-          z += m;
+        for (int e = 0; e < 4; ++e) {
+          const double d = static_cast<double>(x[e]) - dmx;
+          double m = 0.0;
+          if constexpr (decltype(with_z)::value) {
+            m = pow2_neg<!decltype(with_hist)::value>(d * ct, sh.table);  // (exact zeros where step 4 may use the sums)
+            z += m;
+          }
+          if constexpr (decltype(with_z1)::value) z1 += pow2_neg<false>(d * c1, sh.table);
+          if constexpr (decltype(with_hist)::value) {
+            const int b = bin_of(x[e]);
+            if (b < kBins - 1) atomicAdd(&sh.hist[b], by_count ? 1ull : units_of(m));
+          }
         }
-        if (want_conf && !same) z1 += pow2_neg((static_cast<double>(x[e]) - dmx) * c1);
-        if (cut) {
-          const int b = bin_of(x[e]);
-          if (b < kBins - 1)
-            atomicAdd(&sh.hist[b], by_count ? 1ull : static_cast<unsigned long long>(m * kUnit + 0.5));
-        }
-      }
+      });
+    };
+    with_flag(need_z, [&](auto f) EE_ALWAYS_INLINE {
+      with_flag(need_z1, [&](auto g) EE_ALWAYS_INLINE { with_flag(cut, [&](auto h) EE_ALWAYS_INLINE { pass(f, g, h); }); });
     });
     z = block_sum(z);  // (its barrier also closes the histogram)
-    if (want_conf && !same) z1 = block_sum(z1);
+    if (need_z1) z1 = block_sum(z1);
   }
   if (want_conf && tid == 0) {
     const float conf = static_cast<float>(1.0 / (same ? z : z1));
@@ -296,7 +384,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     if (lane == 0) sh.ipart[1][wave] = at;
     __syncthreads();
     if (tid == 0) {
-      for (int w = 0; w < kWaves; ++w) at = min(at, sh.ipart[1][w]);
+      for (int w = 0; w < W; ++w) at = min(at, sh.ipart[1][w]);
       finish(at, 1.0);
     }
     return;
@@ -306,19 +394,17 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   // at least `least`.  The largest logit's first token always is.
   uint32_t tau = 0;
   int ties = 0x7FFFFFFF;
-  const double least = min_p > 0.0f ? (min_p < 1.0f ? static_cast<double>(min_p) : 1.0) : 0.0;
-  const double p = top_p > 0.0f ? static_cast<double>(top_p) : 0.0;
 
   // Inclusive prefix of a value a thread over the block; returns it and the total.
   auto block_scan = [&](auto v, auto *parts, auto &total) EE_ALWAYS_INLINE {
     using V = decltype(v);
-    const V mine = wave_scan(v, lane);
+    const V mine = wave_scan(v);
     if (lane == 63) parts[wave] = mine;
     __syncthreads();
     V before = 0;
     total = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const V t = parts[w];
       if (w < wave) before += t;
       total += t;
@@ -326,58 +412,111 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     __syncthreads();
     return before + mine;
   };
-
-  // Tokens whose bin satisfies lo <= bin <= hi, in the order of ids, as the list;
-  // returns how many there are (the list holds them if no more than it has room for).
-  auto make_list = [&](int lo, int hi) EE_ALWAYS_INLINE {
-    int count = 0;
-    auto in = [&](float x) EE_ALWAYS_INLINE {
-      if (!(x > -INFINITY)) return false;
-      const int b = bin_of(x);
-      return b >= lo && b <= hi;
-    };
-    row.each([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) count += in(x[e]) ? 1 : 0;
-    });
-    count = wave_sum(count);
-    if (lane == 0) sh.ipart[0][wave] = count;
-    __syncthreads();
-    int at = 0, total = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wave) at += sh.ipart[0][w];
-      total += sh.ipart[0][w];
+  struct Block {};
+  struct Wave {};
+  // The same over the block or, where the first wave is alone, over that wave.
+  auto scan = [&](auto scope, auto v, auto &total) EE_ALWAYS_INLINE {
+    using V = decltype(v);
+    if constexpr (std::is_same<decltype(scope), Block>::value) {
+      if constexpr (std::is_same<V, double>::value)
+        return block_scan(v, sh.part[0], total);
+      else
+        return block_scan(v, sh.ipart[0], total);
+    } else {
+      const V mine = wave_scan(v);
+      total = of_lane(mine, 63);
+      return mine;
     }
-    if (total <= kList && count > 0) {
+  };
+  auto sync = [&](auto scope) EE_ALWAYS_INLINE {
+    if constexpr (std::is_same<decltype(scope), Block>::value) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  };
+
+  // Tokens for which in(x) holds, in the order of ids, as the list; returns how many
+  // there are (the list holds them if no more than it has room for).  `give_up`: as soon as
+  // a wave has more than its part of the list, there count as too many.
+  bool again = false;  // in() is asked a second time
+  auto make_list = [&](bool give_up, auto &&in) EE_ALWAYS_INLINE {
+    again = false;
+    constexpr int SEG = kList / W, PER = SEG / 64;
+    static_assert(PER * 64 * W == kList, "whole entries a lane");
+    // The wave's from `at` on, as long as there is room up to `end`; returns how many.
+    auto write = [&](int at, int end) EE_ALWAYS_INLINE {
+      const int begin = at;
       row.each([&](int id, const float (&x)[4]) EE_ALWAYS_INLINE {
-        int mine = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mine += in(x[e]) ? 1 : 0;
-        if (__any(mine > 0)) {
-          const int upto = wave_scan(mine, lane);
-          int o = at + upto - mine;
+        const bool b0 = in(x[0]), b1 = in(x[1]), b2 = in(x[2]), b3 = in(x[3]);
+        if (__any(b0 || b1 || b2 || b3)) {
+          const bool b[4] = {b0, b1, b2, b3};
+          const int upto = wave_scan(static_cast<int>(b0) + b1 + b2 + b3);
+          int o = at + upto - (static_cast<int>(b0) + b1 + b2 + b3);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            if (in(x[e])) {
-              sh.key[o] = key_of(x[e]);
-              sh.id[o] = id + e;
+            if (b[e]) {
+              if (o < end) {
+                sh.key[o] = key_of(x[e]);
+                sh.id[o] = id + e;
+              }
               ++o;
             }
           }
-          at += __shfl(upto, 63);
+          at += of_lane(upto, 63);
+          row.stop = give_up && at > end;
         }
       });
+      const int count = row.stop ? kList + 1 : at - begin;
+      row.stop = false;
+      return count;
+    };
+    // Each wave writes into a part of its own; the parts are then pushed together.
+    const int count = write(wave * SEG, (wave + 1) * SEG);
+    if (lane == 0) sh.ipart[0][wave] = count;
+    __syncthreads();
+    int at = 0, total = 0, most = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const int c = sh.ipart[0][w];
+      if (w < wave) at += c;
+      total += c;
+      most = max(most, c);
+    }
+    if (total <= kList) {
+      if (most <= SEG) {
+        uint32_t k[PER];
+        int d[PER];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          k[e] = sh.key[wave * SEG + e * 64 + lane];
+          d[e] = sh.id[wave * SEG + e * 64 + lane];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          if (e * 64 + lane < count) {
+            sh.key[at + e * 64 + lane] = k[e];
+            sh.id[at + e * 64 + lane] = d[e];
+          }
+        }
+      } else {
+        __syncthreads();  // (a part may reach into the next, whose wave writes it again)
+        again = true;
+        write(at, at + count);
+      }
     }
     __syncthreads();
     return total;
   };
 
-  // The list's keys by falling value in sh.sorted.
-  auto sort_list = [&](int len) EE_ALWAYS_INLINE {
-    int size = 64;
+  // sh.sorted[0 .. len) by falling value: a bitonic network over the next power of two, whose
+  // steps need the block only where they reach past a wave's own 128 keys.
+  auto sort_block = [&](int len) EE_ALWAYS_INLINE {
+    int size = 128;
     while (size < len) size <<= 1;
-    for (int i = tid; i < size; i += kThreads) sh.sorted[i] = i < len ? sh.key[i] : 0;
+    for (int i = len + tid; i < size; i += kThreads) sh.sorted[i] = 0;
     __syncthreads();
     for (int k = 2; k <= size; k <<= 1) {
       for (int j = k >> 1; j > 0; j >>= 1) {
@@ -390,41 +529,116 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
             sh.sorted[o] = x;
           }
         }
-        __syncthreads();
+        const int next = j > 1 ? j >> 1 : k;
+        if (j > 64 || next > 64)
+          __syncthreads();
+        else
+          sync(Wave{});
       }
     }
+    __syncthreads();
+  };
+  // The same for up to 128 keys of the list, by one wave: for each those before it counted.
+  auto sort_wave = [&](int len) EE_ALWAYS_INLINE {
+    for (int i = lane; i < len; i += 64) {
+      const uint32_t mine = sh.key[i];
+      int rank = 0;
+      for (int j = 0; j < len; ++j) {
+        const uint32_t k = sh.key[j];
+        rank += k > mine || (k == mine && j < i) ? 1 : 0;
+      }
+      sh.sorted[rank] = mine;
+    }
+    sync(Wave{});
   };
 
-  // tau and ties from the sorted list of `len` keys: of the first `most`, those
-  // before which less than the target has gathered (share < 0: of p times the
-  // mass of the first `most`; else `share`).
-  auto cut_list = [&](int len, int most, double share) EE_ALWAYS_INLINE {
-    double m[4], sum = 0.0, total;
-    uint32_t k[4];
+  // tau and ties from `len` sorted keys: of the first `most`, those before which less than the
+  // target has gathered (share_of < 0: of p times the mass of the first `most`; else share_of).
+  auto cut_sorted = [&](auto scope, int len, int most, double share_of) EE_ALWAYS_INLINE {
+    constexpr int PER = std::is_same<decltype(scope), Block>::value ? kSorted / kThreads : kSmallList / 64;
+    double m[PER], sum = 0.0, total;
+    uint32_t k[PER];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = tid * 4 + e;
+    for (int e = 0; e < PER; ++e) {
+      const int i = tid * PER + e;
       k[e] = i < len ? sh.sorted[i] : 0;
-      m[e] = i < most ? mass_of(value_of(k[e])) : 0.0;
+      m[e] = by_mass && i < most ? mass_of(value_of(k[e])) : 0.0;
       sum += m[e];
     }
-    double before = block_scan(sum, sh.part[0], total) - sum;
-    const double target = !by_mass ? INFINITY : share < 0.0 ? p * total : share;
+    double before = scan(scope, sum, total) - sum;
+    const double target = !by_mass ? INFINITY : share_of < 0.0 ? p * total : share_of;
     int keep = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = tid * 4 + e;
+    for (int e = 0; e < PER; ++e) {
+      const int i = tid * PER + e;
       if (i < most && (i == 0 || before < target)) ++keep;
       before += m[e];
     }
     int kept;
-    block_scan(keep, sh.ipart[0], kept);
+    scan(scope, keep, kept);
     tau = sh.sorted[kept - 1];
     int above = 0, n_above;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) above += tid * 4 + e < kept && k[e] > tau ? 1 : 0;
-    block_scan(above, sh.ipart[0], n_above);
+    for (int e = 0; e < PER; ++e) above += tid * PER + e < kept && k[e] > tau ? 1 : 0;
+    scan(scope, above, n_above);
     ties = kept - n_above;
+  };
+
+  // The token from a list that holds all that is kept.
+  auto pick_listed = [&](auto scope, int len) EE_ALWAYS_INLINE {
+    constexpr bool BLOCK = std::is_same<decltype(scope), Block>::value;
+    constexpr int PER = BLOCK ? kList / kThreads : kSmallList / 64;
+    double m[PER], sum = 0.0, total;
+    int tie = 0, n_tie;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) tie += tid * PER + e < len && sh.key[tid * PER + e] == tau ? 1 : 0;
+    int rank = scan(scope, tie, n_tie) - tie;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const int i = tid * PER + e;
+      m[e] = 0.0;
+      if (i < len) {
+        const uint32_t k = sh.key[i];
+        const bool in = k > tau || (k == tau && rank < ties);
+        if (k == tau) ++rank;
+        if (in) {
+          m[e] = mass_of(value_of(k));
+          if (m[e] < least) m[e] = 0.0;
+        }
+      }
+      sum += m[e];
+    }
+    double upto = scan(scope, sum, total) - sum;
+    const double goal = static_cast<double>(u) * total;
+    // the first that passes the goal; if none does (u of 1 and more), the last that has mass
+    int first = 0x7FFFFFFF, last = -1;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      upto += m[e];
+      if (m[e] > 0.0) {
+        last = tid * PER + e;
+        if (upto > goal && first == 0x7FFFFFFF) first = tid * PER + e;
+      }
+    }
+    const uint64_t firsts = __ballot(first != 0x7FFFFFFF), lasts = __ballot(last >= 0);
+    first = firsts != 0 ? of_lane(first, __builtin_ctzll(firsts)) : 0x7FFFFFFF;
+    last = lasts != 0 ? of_lane(last, 63 - __builtin_clzll(lasts)) : -1;
+    if constexpr (BLOCK) {
+      if (lane == 0) {
+        sh.ipart[0][wave] = first;
+        sh.ipart[1][wave] = last;
+      }
+      __syncthreads();
+      if (tid != 0) return;
+      for (int w = 0; w < W; ++w) {
+        first = min(first, sh.ipart[0][w]);
+        last = max(last, sh.ipart[1][w]);
+      }
+    }
+    if (tid == 0) {
+      const int at = first != 0x7FFFFFFF ? first : last;
+      finish(sh.id[at], mass_of(value_of(sh.key[at])) / total);
+    }
   };
 
   // tau by the digits of the keys: the largest key with at least `target` tokens, or
@@ -432,12 +646,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
   auto cut_digits = [&](bool count, double target, double &above) EE_ALWAYS_INLINE {
     uint32_t prefix = 0;
     double over = 0.0;
-    const int bits[3] = {11, 11, 10};
     int shift = 32;
     for (int d = 0; d < 3; ++d) {
       const uint32_t mask = shift == 32 ? 0 : ~0u << shift;
-      const int nb = 1 << bits[d];
-      shift -= bits[d];
+      const int nb = d < 2 ? 2048 : 1024;
+      shift -= d < 2 ? 11 : 10;
       for (int i = tid; i < nb; i += kThreads) sh.hist[i] = 0;
       __syncthreads();
       row.each([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
@@ -445,35 +658,37 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
         for (int e = 0; e < 4; ++e) {
           const uint32_t key = key_of(x[e]);
           if (x[e] > -INFINITY && (key & mask) == (prefix & mask))
-            atomicAdd(&sh.hist[(key >> shift) & (nb - 1)],
-                      count ? 1ull : static_cast<unsigned long long>(mass_of(x[e]) * kUnit + 0.5));
+            atomicAdd(&sh.hist[(key >> shift) & (nb - 1)], count ? 1ull : units_of(mass_of(x[e])));
         }
       });
       __syncthreads();
-      // bins from the top: thread t has bins nb - 1 - 2 t and nb - 2 - 2 t
-      const int hi = nb - 1 - 2 * tid;
-      const unsigned long long v0 = hi >= 0 ? sh.hist[hi] : 0, v1 = hi >= 1 ? sh.hist[hi - 1] : 0;
+      // bins from the top: thread t has the PB bins from nb - 1 - PB t down
+      constexpr int PB = kBins / kThreads;
+      const int hi = nb - 1 - PB * tid;
+      unsigned long long v[PB], sum = 0, total;
+      int low = 0x7FFFFFFF;
+#pragma unroll
+      for (int e = 0; e < PB; ++e) {
+        v[e] = hi - e >= 0 ? sh.hist[hi - e] : 0;
+        sum += v[e];
+        if (v[e] > 0) low = hi - e;
+      }
       if (tid == 0) sh.found = -1;
-      unsigned long long total;
-      const unsigned long long upto = block_scan(v0 + v1, sh.upart, total);
       const double unit = count ? 1.0 : 1.0 / kUnit;
-      const double b0 = over + static_cast<double>(upto - v0 - v1) * unit, b1 = over + static_cast<double>(upto - v1) * unit,
-                   b2 = over + static_cast<double>(upto) * unit;
-      if (hi >= 0 && v0 > 0 && b0 < target && b1 >= target) {
-        sh.found = hi;
-        sh.before = upto - v0 - v1;
-      } else if (hi >= 1 && v1 > 0 && b1 < target && b2 >= target) {
-        sh.found = hi - 1;
-        sh.before = upto - v1;
+      unsigned long long before = block_scan(sum, sh.upart, total) - sum;
+#pragma unroll
+      for (int e = 0; e < PB; ++e) {
+        if (v[e] > 0 && over + static_cast<double>(before) * unit < target && over + static_cast<double>(before + v[e]) * unit >= target) {
+          sh.found = hi - e;
+          sh.before = before;
+        }
+        before += v[e];
       }
       __syncthreads();
       int f = sh.found;
       unsigned long long lower = sh.before;
       if (f < 0) {  // the whole row does not reach the target (or masses below the unit): its last bin
         __syncthreads();
-        int low = 0x7FFFFFFF;
-        if (hi >= 0 && v0 > 0) low = hi;
-        if (hi >= 1 && v1 > 0) low = hi - 1;
         if (low != 0x7FFFFFFF) atomicMax(&sh.found, 0x7FFFFFFF - low);
         __syncthreads();
         f = sh.found < 0 ? 0 : 0x7FFFFFFF - sh.found;
@@ -487,34 +702,107 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     above = over;
   };
 
-  bool listed = false;  // the list holds all that is kept
-  int len = 0;
+  bool in_bin = false;
+  double above_bin = 0.0;
   if (cut) {
     // 3. the bin of the cut: the first at which the gathered counts or masses reach the target
+    constexpr int PB = kBins / kThreads;
     const double target = by_count ? static_cast<double>(top_k) : p * z * kUnit;
-    const unsigned long long v0 = sh.hist[2 * tid], v1 = 2 * tid + 1 < kBins - 1 ? sh.hist[2 * tid + 1] : 0;
+    unsigned long long v[PB], sum = 0, total;
+#pragma unroll
+    for (int e = 0; e < PB; ++e) {
+      v[e] = tid * PB + e < kBins - 1 ? sh.hist[tid * PB + e] : 0;
+      sum += v[e];
+    }
     if (tid == 0) sh.found = kBins - 1;
-    unsigned long long total;
-    const unsigned long long upto = block_scan(v0 + v1, sh.upart, total);
-    const double b0 = static_cast<double>(upto - v0 - v1), b1 = static_cast<double>(upto - v1), b2 = static_cast<double>(upto);
-    if ((tid == 0 || b0 < target) && b1 >= target) {
-      sh.found = 2 * tid;
-      sh.before = upto - v0 - v1;
-    } else if (b1 < target && b2 >= target) {
-      sh.found = 2 * tid + 1;
-      sh.before = upto - v1;
+    unsigned long long before = block_scan(sum, sh.upart, total) - sum;
+#pragma unroll
+    for (int e = 0; e < PB; ++e) {
+      const int b = tid * PB + e;
+      if ((b == 0 || static_cast<double>(before) < target) && static_cast<double>(before + v[e]) >= target && b < kBins - 1) {
+        sh.found = b;
+        sh.before = before;
+      }
+      before += v[e];
     }
     __syncthreads();
     const int bin = sh.found;
     const double lower = static_cast<double>(sh.before) / kUnit;
-    len = make_list(0, bin);
+    // All that lies in the bin and above, by one comparison: the bin's lower edge,
+    // moved down past what its rounding may hide (a few tokens more do no harm).
+    const float edge = (mx - static_cast<float>(bin + 1) / bscale), from = edge - 1e-5f * (fabsf(edge) + fabsf(mx));
+    const bool all = bin == kBins - 1 || !(from > -INFINITY);
+    int len = make_list(!by_count, [&](float x) EE_ALWAYS_INLINE { return all ? x > -INFINITY : x >= from; });
+    if (len <= kSmallList) {
+      if (wave == 0) {
+        sort_wave(len);
+        cut_sorted(Wave{}, len, by_count ? min(top_k, len) : len, by_count ? -1.0 : p * z);
+        pick_listed(Wave{}, len);
+      }
+      return;
+    }
     if (len <= kList) {
-      listed = true;
-      sort_list(len);
-      cut_list(len, by_count ? min(top_k, len) : len, by_count ? -1.0 : p * z);
-    } else if (!by_count && bin < kBins - 1 && (len = make_list(bin, bin)) <= kList) {
-      sort_list(len);
-      cut_list(len, len, p * z - lower);
+      // With one criterion only the cut's bin has to be sorted: what lies above it is known.
+      const bool whole = by_count && by_mass, tail = bin == kBins - 1;
+      const int above_bin_count = static_cast<int>(sh.before);
+      if (tid == 0) sh.n_sub = 0;
+      __syncthreads();
+      for (int i = tid; i < len; i += kThreads) {
+        const uint32_t k = sh.key[i];
+        if (whole || tail || bin_of(value_of(k)) == bin) {
+          const int at = atomicAdd(&sh.n_sub, 1);  // (in any order: they are sorted next)
+          if (at < kSorted) sh.sorted[at] = k;
+        }
+      }
+      __syncthreads();
+      const int n_sub = sh.n_sub;
+      if (n_sub <= kSorted) {
+        sort_block(n_sub);
+        if (whole || tail)
+          cut_sorted(Block{}, n_sub, by_count ? min(top_k, n_sub) : n_sub, by_count ? -1.0 : p * z);
+        else
+          cut_sorted(Block{}, n_sub, by_count ? min(top_k - above_bin_count, n_sub) : n_sub, p * z - lower);
+        pick_listed(Block{}, len);
+        return;
+      }
+    }
+    if (!by_count && bin < kBins - 1) {
+      // the bin's tokens, and on the way the mass that each wave has above it
+      len = make_list(false, [&](float x) EE_ALWAYS_INLINE {
+        if (!(x > -INFINITY)) return false;
+        const int b = bin_of(x);
+        if (b < bin && !again) above_bin += mass_of(x);
+        return b == bin;
+      });
+      in_bin = len <= min(kList, kSorted);
+    }
+    if (in_bin) {
+      for (int i = tid; i < len; i += kThreads) sh.sorted[i] = sh.key[i];
+      sort_block(len);
+      cut_sorted(Block{}, len, len, p * z - lower);
+      above_bin = wave_sum(above_bin);
+      // the list is in the order of ids: the wave's part of it, and what of it is kept
+      int lo = 0, hi = 0;
+      for (int i = lane; i < len; i += 64) {
+        lo += sh.id[i] < row.first ? 1 : 0;
+        hi += sh.id[i] < row.last ? 1 : 0;
+      }
+      lo = wave_sum(lo);
+      hi = wave_sum(hi);
+      double m = 0.0;
+      int tie = 0;
+      for (int i = lo + lane; i < hi; i += 64) {
+        const uint32_t k = sh.key[i];
+        if (k > tau) m += mass_of(value_of(k));
+        if (k == tau) ++tie;
+      }
+      m = wave_sum(m);
+      tie = wave_sum(tie);
+      if (lane == 0) {
+        sh.part[0][wave] = above_bin + m;
+        sh.ipart[0][wave] = tie;
+      }
+      __syncthreads();
     } else {
       double above;
       if (by_count) {
@@ -544,110 +832,78 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     }
   }
 
-  if (listed) {
-    // the token from the list, which is in the order of ids
-    double m[4], sum = 0.0, total;
-    int tie = 0, n_tie;
+  // The token from the row: each wave's kept mass, the wave in whose share the goal lies,
+  // then the same once more with that share divided among all waves, and that wave's ids one
+  // by one.
+  const double q = mass_of(value_of(tau)), tie_mass = q >= least ? q : 0.0;
+  // What the waves have is known from step 2 (slot 1, no ties), or from the list of the
+  // cut's bin, unless min-p takes some of it away again.
+  const bool from_sums = !cut && least == 0.0, from_list = in_bin && least == 0.0;
+  double before = 0.0, goal = 0.0, total = 0.0;
+  int ties_before = 0, from = 0, width = chunk;
+  for (int level = 0; level < 2; ++level) {
+    const bool summed = level == 0 && from_sums;
+    if (!summed && !(level == 0 && from_list)) {
+      double m = 0.0;
+      int tie = 0;
+      row.each([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) tie += tid * 4 + e < len && sh.key[tid * 4 + e] == tau ? 1 : 0;
-    int rank = block_scan(tie, sh.ipart[0], n_tie) - tie;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int i = tid * 4 + e;
-      m[e] = 0.0;
-      if (i < len) {
-        const uint32_t k = sh.key[i];
-        const bool in = k > tau || (k == tau && rank < ties);
-        if (k == tau) ++rank;
-        if (in) {
-          m[e] = mass_of(value_of(k));
-          if (m[e] < least) m[e] = 0.0;
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t k = key_of(x[e]);
+          if (x[e] > -INFINITY) {
+            if (k > tau) {
+              const double v = mass_of(x[e]);
+              m += v >= least ? v : 0.0;
+            } else if (k == tau) {
+              ++tie;
+            }
+          }
         }
+      });
+      m = wave_sum(m);
+      tie = wave_sum(tie);
+      __syncthreads();  // nobody reads the slots any more
+      if (lane == 0) {
+        sh.part[0][wave] = m;
+        sh.ipart[0][wave] = tie;
       }
-      sum += m[e];
+      __syncthreads();
     }
-    double upto = block_scan(sum, sh.part[0], total) - sum;
-    const double goal = static_cast<double>(u) * total;
-    // the first that passes the goal; if none does (u of 1 and more), the last that has mass
-    int first = 0x7FFFFFFF, last = -1;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      upto += m[e];
-      if (m[e] > 0.0) {
-        last = tid * 4 + e;
-        if (upto > goal && first == 0x7FFFFFFF) first = tid * 4 + e;
+    // (step 2 left its sums, which have no ties, in slot 1)
+    auto wave_of = [&](int w, int seen, int &t) EE_ALWAYS_INLINE {
+      t = summed ? 0 : sh.ipart[0][w];
+      return sh.part[summed ? 1 : 0][w] + min(max(ties - seen, 0), t) * tie_mass;
+    };
+    int t;
+    if (level == 0) {
+      for (int w = 0, seen = 0; w < W; ++w) {
+        total += wave_of(w, seen, t);
+        seen += t;
       }
+      goal = static_cast<double>(u) * total;
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      first = min(first, __shfl_xor(first, o));
-      last = max(last, __shfl_xor(last, o));
-    }
-    if (lane == 0) {
-      sh.ipart[0][wave] = first;
-      sh.ipart[1][wave] = last;
-    }
-    __syncthreads();
-    if (tid == 0) {
-      for (int w = 0; w < kWaves; ++w) {
-        first = min(first, sh.ipart[0][w]);
-        last = max(last, sh.ipart[1][w]);
+    int pick = -1;
+    double upto = before;
+    for (int w = 0, seen = ties_before; w < W; ++w) {
+      const double mass = wave_of(w, seen, t);
+      if (mass > 0.0 && (pick < 0 || upto <= goal)) {
+        pick = w;
+        before = upto;
+        ties_before = seen;
       }
-      const int at = first != 0x7FFFFFFF ? first : last;
-      finish(sh.id[at], mass_of(value_of(sh.key[at])) / total);
+      upto += mass;
+      seen += t;
     }
-    return;
-  }
-
-  // the token from the row: kept mass and ties of each wave, then the wave that has it
-  double m = 0.0;
-  int tie = 0;
-  const double q = mass_of(value_of(tau));
-  row.each([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t k = key_of(x[e]);
-      if (x[e] > -INFINITY) {
-        if (k > tau) {
-          const double v = mass_of(x[e]);
-          m += v >= least ? v : 0.0;
-        } else if (k == tau) {
-          ++tie;
-        }
-      }
+    from = from + pick * width;
+    const int to = min(from + width, a.vocab);
+    if (level == 0) {
+      width = share(from, to);
+    } else {
+      if (wave != 0) return;
+      row.first = from;
+      row.last = to;
     }
-  });
-  m = wave_sum(m);
-  tie = wave_sum(tie);
-  if (lane == 0) {  // (slots that no wave may still be reading)
-    sh.part[slot][wave] = m;
-    sh.ipart[1][wave] = tie;
   }
-  __syncthreads();
-  const double tie_mass = q >= least ? q : 0.0;
-  double total = 0.0, wave_mass[kWaves];
-  int seen = 0, ties_before = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const int mine = min(max(ties - seen, 0), sh.ipart[1][w]);
-    wave_mass[w] = sh.part[slot][w] + mine * tie_mass;
-    if (w == wave) ties_before = seen;
-    seen += sh.ipart[1][w];
-    total += wave_mass[w];
-  }
-  const double goal = static_cast<double>(u) * total;
-  int pick = -1;
-  double start = 0.0, sum = 0.0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (wave_mass[w] > 0.0 && (pick < 0 || sum <= goal)) {
-      pick = w;
-      start = sum;
-    }
-    sum += wave_mass[w];
-  }
-  if (wave != pick) return;
-  double before = start, chosen_mass = 0.0;
   int rank = ties_before, chosen = -1;
   bool done = false;
   row.each([&](int id, const float (&x)[4]) EE_ALWAYS_INLINE {
@@ -655,7 +911,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
     int mine = 0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) mine += x[e] > -INFINITY && key_of(x[e]) == tau ? 1 : 0;
-    const int t_upto = wave_scan(mine, lane);
+    const int t_upto = wave_scan(mine);
     int r = rank + t_upto - mine;
     double v[4], s = 0.0;
 #pragma unroll
@@ -669,50 +925,59 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleArgs a) {
       }
       s += v[e];
     }
-    double upto = wave_scan(s, lane);
-    const double iter = __shfl(upto, 63);
+    double upto = wave_scan(s);
+    const double iter = of_lane(upto, 63);
     upto += before - s;
     int hit = -1, last = -1;
-    double hit_mass = 0.0, last_mass = 0.0;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       upto += v[e];
       if (v[e] > 0.0) {
         last = id + e;
-        last_mass = v[e];
-        if (hit < 0 && upto > goal) {
-          hit = id + e;
-          hit_mass = v[e];
-        }
+        if (hit < 0 && upto > goal) hit = id + e;
       }
     }
     const uint64_t hits = __ballot(hit >= 0), lasts = __ballot(last >= 0);
     if (hits != 0) {
-      const int l = __builtin_ctzll(hits);
-      chosen = __shfl(hit, l);
-      chosen_mass = __shfl(hit_mass, l);
+      chosen = of_lane(hit, __builtin_ctzll(hits));
       done = true;
     } else if (lasts != 0) {
-      const int l = 63 - __builtin_clzll(lasts);
-      chosen = __shfl(last, l);
-      chosen_mass = __shfl(last_mass, l);
+      chosen = of_lane(last, 63 - __builtin_clzll(lasts));
     }
     before += iter;
-    rank += __shfl(t_upto, 63);
+    rank += of_lane(t_upto, 63);
   });
-  if (lane == 0) finish(chosen, chosen_mass / total);
+  if (lane == 0) finish(chosen, mass_of(to_f32(row.p[chosen])) / total);
 }
 
 }  // namespace
+
+// The largest row that LDS holds beside what else is there: 32000 fp32 logits.
+constexpr size_t kLds = 160 << 10;
 
 size_t sample_workspace(int, int) { return 256; }
 
 hipError_t launch_sample(bool f32, const SampleArgs &a, void *, hipStream_t stream) {
   if (a.n <= 0) return hipSuccess;
+  const size_t row = (static_cast<size_t>(a.vocab) + 3) / 4 * 4 * (f32 ? 4 : 2);
+  const bool cached = shared_bytes(true) + row <= kLds;
+  const size_t lds = shared_bytes(cached) + (cached ? row : 0);
+  hipError_t e = hipSuccess;
   EE_DISPATCH(f32, {
-    hipLaunchKernelGGL((sample_kernel<T, 0>), dim3(a.n), dim3(kThreads), 0, stream, a);
+    auto go = [&](auto k, int waves) {
+      e = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
+      if (e != hipSuccess) return;
+      hipLaunchKernelGGL(k, dim3(a.n), dim3(64 * waves), lds, stream, a);
+      e = hipGetLastError();
+    };
+    if (cached)
+      go(sample_kernel<T, true, 16>, 16);
+    else if (a.n > 256)
+      go(sample_kernel<T, false, 8>, 8);
+    else
+      go(sample_kernel<T, false, 16>, 16);
   });
-  return hipGetLastError();
+  return e;
 }
 
 }  // namespace ee
