@@ -139,8 +139,13 @@ struct StoreC {
   void *c;
   int64_t ld;
   int rows, features;
-  bool accumulate, vec;  // vec: groups of four features are aligned
+  bool accumulate, vec, vec8;  // vec, vec8: groups of four (eight) features are aligned
 };
+
+__device__ __forceinline__ u32x2_t pack4(f32x4_t v) {
+  return u32x2_t{static_cast<uint32_t>(f32_to_bf16(v[0])) | (static_cast<uint32_t>(f32_to_bf16(v[1])) << 16),
+                 static_cast<uint32_t>(f32_to_bf16(v[2])) | (static_cast<uint32_t>(f32_to_bf16(v[3])) << 16)};
+}
 
 // Four consecutive features of one row of C.
 template <bool F32>
@@ -160,9 +165,7 @@ __device__ __forceinline__ void store_c(const StoreC &s, int row, int f, f32x4_t
   } else {
     bf16_t *p = static_cast<bf16_t *>(s.c) + o;
     if (s.vec && f + 4 <= s.features) {
-      *reinterpret_cast<u32x2_t *>(p) =
-          u32x2_t{static_cast<uint32_t>(f32_to_bf16(v[0])) | (static_cast<uint32_t>(f32_to_bf16(v[1])) << 16),
-                  static_cast<uint32_t>(f32_to_bf16(v[2])) | (static_cast<uint32_t>(f32_to_bf16(v[3])) << 16)};
+      *reinterpret_cast<u32x2_t *>(p) = pack4(v);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -170,6 +173,23 @@ __device__ __forceinline__ void store_c(const StoreC &s, int row, int f, f32x4_t
     }
   }
 }
+
+// Eight consecutive features of one row of a bf16 C.
+__device__ __forceinline__ void store_row8(const StoreC &s, int row, int f, u32x4_t v) {
+  if (row >= s.rows || f >= s.features) return;
+  bf16_t *p = static_cast<bf16_t *>(s.c) + static_cast<int64_t>(row) * s.ld + f;
+  if (s.vec8 && f + 8 <= s.features) {
+    *reinterpret_cast<u32x4_t *>(p) = v;
+  } else {
+    static_for<8>([&](auto e) EE_ALWAYS_INLINE {
+      constexpr int E = decltype(e)::value;
+      if (f + E < s.features) p[E] = static_cast<bf16_t>(v[E / 2] >> (16 * (E % 2)));
+    });
+  }
+}
+
+// The 32 bytes of a row that a lane holds as two fragments of 16.
+__device__ __forceinline__ i32x8_t fragment(const bf16x8_t (&f)[2]) { return __builtin_bit_cast(i32x8_t, f); }
 
 // Ring of NS stages, the stage NS - 1 further on loaded while one is consumed, one
 // barrier a stage (as Ring of ring.h).  W: the rows operand, Z: the columns.  ROW1: W's
@@ -282,6 +302,190 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void ring8_kernel(ScaledM
   });
 }
 
+// bf16 C, weights with 128 x 128 blocks: 256 x 256 tiles on 8 waves of 128 features x 64
+// tokens, the phases of GemmBlockBig (gemm.h) with stages of 128 codes in place of 64 bf16
+// values.  A wave's 128 features are one block of the weight's scales, its lanes' tokens
+// have one scale each, so a stage needs four scale products a lane.  The scales of a stage
+// (256 features', 256 tokens') take one more load a thread, into one of four places in LDS.
+constexpr int kBigStages = 131072, kBigScales = 2048;
+
+template <bool E5>
+__global__ __launch_bounds__(512, 1) void big8_kernel(ScaledMat W, ScaledMat Z, int K, StoreC out) {
+  __shared__ __attribute__((aligned(128))) char smem[kBigStages + 4 * kBigScales];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wave_m = wave >> 2, wave_n = wave & 3;
+  int tile_m, tile_n;
+  tile_of_block(blockIdx.x, gridDim.x, cdiv(W.rows, 256), cdiv(Z.rows, 256), tile_m, tile_n);
+  const int m0 = tile_m * 256, n0 = tile_n * 256;
+  const int bytes = (K + 15) & ~15, nk = bytes / 128;  // whole stages
+  constexpr int B_OFF = 32768;
+  TileOperandB16<true, 128, false, false> ta;
+  TileOperandB16<true, 64, false, false> tb;
+  ta.init(Operand{W.data, W.ld / 2}, m0, W.rows, 0, tid, wave_m, lane, smem);
+  tb.init(Operand{Z.data, Z.ld / 2}, n0, Z.rows, 0, tid, wave_n, lane, smem + B_OFF);
+  const uint32_t lds0 =
+      static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)smem));
+  const uint32_t lds_wave = lds0 + wave * 1024;
+  const ScaledMat &side = wave < 4 ? W : Z;  // whose scales this wave loads
+  const char *sbase = reinterpret_cast<const char *>(side.scale);
+  const uint32_t soff =
+      static_cast<uint32_t>(min((wave < 4 ? m0 + tid : n0 + tid - 256), side.rows - 1) >> side.shift) * 4;
+  const int64_t sstep = side.scale_ld * 4;
+  auto load_s = [&](int t, int u) EE_ALWAYS_INLINE {  // stage u's, to stage t's place
+    load_lds4(sbase + u * sstep, soff, lds0 + kBigStages + (t & 3) * kBigScales + wave * 256);
+  };
+  auto load_a = [&](auto q, auto buf, int t) EE_ALWAYS_INLINE {
+    ta.template load<decltype(q)::value>(min(t, nk - 1), 64, lds_wave + decltype(buf)::value * 65536);
+  };
+  auto load_b = [&](auto q, auto buf, int t) EE_ALWAYS_INLINE {
+    tb.template load<decltype(q)::value>(min(t, nk - 1), 64, lds_wave + decltype(buf)::value * 65536 + B_OFF);
+  };
+  f32x4_t acc[8][4];
+  static_for<8>([&](auto i) EE_ALWAYS_INLINE {
+    static_for<4>([&](auto j) EE_ALWAYS_INLINE { acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}; });
+  });
+  bf16x8_t fa[4][2], fb[2][2][2];
+  float zs[4];
+  auto read_s = [&](int t) EE_ALWAYS_INLINE {
+    const float *sc = reinterpret_cast<const float *>(smem + kBigStages + (t & 3) * kBigScales);
+    const float ws = sc[wave_m * 128];
+    static_for<4>([&](auto j) EE_ALWAYS_INLINE {
+      zs[j] = ws * sc[256 + wave_n * 64 + decltype(j)::value * 16 + (lane & 15)];
+    });
+  };
+  // One quadrant: eight products, each added two products later, so that the scaled adds
+  // run under the matrix instructions.
+  auto mma = [&](auto qa, auto qb) EE_ALWAYS_INLINE {
+    f32x4_t d[8];
+    static_for<10>([&](auto n) EE_ALWAYS_INLINE {
+      constexpr int N = decltype(n)::value;
+      if constexpr (N < 8) d[N] = mfma8<E5>(fragment(fa[N / 2]), fragment(fb[qb][N % 2]));
+      if constexpr (N >= 2) {
+        constexpr int P = N - 2, I = decltype(qa)::value * 4 + P / 2, J = decltype(qb)::value * 2 + P % 2;
+        acc[I][J] += d[P] * zs[J];
+      }
+    });
+  };
+  using H0 = std::integral_constant<int, 0>;
+  using H1 = std::integral_constant<int, 1>;
+  load_s(0, 0);
+  load_b(H0{}, H0{}, 0);
+  load_a(H0{}, H0{}, 0);
+  load_b(H1{}, H0{}, 0);
+  load_a(H1{}, H0{}, 0);
+  load_s(1, min(1, nk - 1));
+  load_b(H1{}, H1{}, 1);
+  load_a(H0{}, H1{}, 1);
+  load_b(H0{}, H1{}, 1);
+  load_a(H1{}, H1{}, 1);
+  wait_vm<13>();  // stage 0's scales and first halves
+  phase_barrier();
+  tb.template read<0, 0>(fb[0]);
+  wait_lgkm();
+  phase_barrier();
+  if (wave_m == 1) phase_barrier();  // waves 4..7 run one barrier behind
+  // As GemmBlockBig's stage; the loads past which a wait lets none through are the last six
+  // halves' and the scales' among them.
+  auto stage = [&](auto buf, int t) EE_ALWAYS_INLINE {
+    constexpr int BUF = decltype(buf)::value;
+    using Cur = std::integral_constant<int, BUF>;
+    using First = Cur;
+    using Second = std::integral_constant<int, BUF ^ 1>;
+    read_s(t);
+    ta.template read<BUF, 0>(fa);
+    load_b(First{}, Cur{}, t + 2);
+    load_s(t + 2, min(t + 2, nk - 1));
+    wait_vm<14>();
+    wait_lgkm();
+    phase_barrier();
+    mma(H0{}, First{});
+    phase_barrier();
+    tb.template read<BUF, BUF ^ 1>(fb[BUF ^ 1]);
+    load_a(H0{}, Cur{}, t + 2);
+    wait_vm<14>();
+    wait_lgkm();
+    phase_barrier();
+    mma(H0{}, Second{});
+    phase_barrier();
+    ta.template read<BUF, 1>(fa);
+    load_b(Second{}, Cur{}, t + 2);
+    wait_vm<13>();
+    wait_lgkm();
+    phase_barrier();
+    mma(H1{}, Second{});
+    phase_barrier();
+    tb.template read<BUF ^ 1, BUF ^ 1>(fb[BUF ^ 1]);
+    load_a(H1{}, Cur{}, t + 2);
+    wait_vm<13>();
+    wait_lgkm();
+    phase_barrier();
+    mma(H1{}, First{});
+    phase_barrier();
+  };
+  int t = 0;
+  for (; t + 1 < nk; t += 2) {
+    stage(H0{}, t);
+    stage(H1{}, t + 1);
+  }
+  if (t < nk) stage(H0{}, t);
+  if (wave_m == 0) phase_barrier();
+  wait_vm<0>();
+  phase_barrier();
+  const int left = bytes - nk * 128;
+  if (left > 0) {  // codes past the last whole stage: a stage of its own, zero from there on
+    const int ch = (tid & 7) ^ ((tid >> 4) & 7);
+    const bool past = ch * 16 >= left;
+    auto tail = [&](auto &op, int at) EE_ALWAYS_INLINE {
+      static_for<2>([&](auto h) EE_ALWAYS_INLINE {
+        static_for<2>([&](auto e) EE_ALWAYS_INLINE {
+          constexpr int H = decltype(h)::value, E = decltype(e)::value;
+          load_lds16(op.base + static_cast<int64_t>(nk) * 128, past ? op.off[H][E] - ch * 16 : op.off[H][E],
+                     lds_wave + at + H * 16384 + E * 8192);
+        });
+      });
+    };
+    tail(ta, 0);
+    tail(tb, B_OFF);
+    load_s(0, nk);
+    wait_vm<0>();
+    if (past) {
+      static_for<8>([&](auto e) EE_ALWAYS_INLINE {
+        *reinterpret_cast<u32x4_t *>(smem + decltype(e)::value * 8192 + tid * 16) = u32x4_t{0, 0, 0, 0};
+      });
+    }
+    wait_lgkm();
+    phase_barrier();
+    read_s(0);
+    tb.template read<0, 0>(fb[0]);
+    tb.template read<0, 1>(fb[1]);
+    static_for<2>([&](auto qa) EE_ALWAYS_INLINE {
+      ta.template read<0, decltype(qa)::value>(fa);
+      mma(qa, H0{});
+      mma(qa, H1{});
+    });
+    wait_lgkm();
+    phase_barrier();
+  }
+  // C through LDS, a wave's 64 rows of 128 features (256 bytes) in 16 KB of its own: 16-byte
+  // chunk c of row r at c ^ (r mod 16), so that it leaves in whole lines.
+  char *mine = smem + wave * 16384;
+  static_for<8>([&](auto i) EE_ALWAYS_INLINE {
+    static_for<4>([&](auto j) EE_ALWAYS_INLINE {
+      constexpr int I = decltype(i)::value, J = decltype(j)::value;
+      const f32x4_t v = acc[I][J];
+      const int r = J * 16 + (lane & 15), g = lane >> 4;
+      *reinterpret_cast<u32x2_t *>(mine + r * 256 + (((2 * I + (g >> 1)) ^ (r & 15)) << 4) + (g & 1) * 8) = pack4(v);
+    });
+  });
+  wait_lgkm();
+  const int row0 = n0 + wave_n * 64, f0 = m0 + wave_m * 128;
+  static_for<16>([&](auto it) EE_ALWAYS_INLINE {
+    const int r = decltype(it)::value * 4 + (lane >> 4), c = lane & 15, f = f0 + c * 8;
+    const u32x4_t v = *reinterpret_cast<const u32x4_t *>(mine + r * 256 + ((c ^ (r & 15)) << 4));
+    store_row8(out, row0 + r, f, v);
+  });
+}
+
 template <int BM, int BN, int WM, int WN, int NS>
 hipError_t launch_ring8(const ScaledMat &W, const ScaledMat &Z, bool f32, const StoreC &out, hipStream_t stream) {
   const int64_t blocks = static_cast<int64_t>(cdiv(W.rows, BM)) * cdiv(Z.rows, BN);
@@ -313,10 +517,18 @@ hipError_t scaled_matmul(const ScaledMat &a, const ScaledMat &b, void *c, bool c
                          hipStream_t stream) {
   if (a.rows <= 0 || b.rows <= 0) return hipSuccess;
   if (((a.cols + 15) & ~15) != ((b.cols + 15) & ~15) || b.e5m2) return hipErrorInvalidValue;
-  const StoreC out{c, ldc, a.rows, b.rows, accumulate != 0, ldc % 4 == 0};
+  const StoreC out{c, ldc, a.rows, b.rows, accumulate != 0, ldc % 4 == 0, ldc % 8 == 0};
+  if (!c_f32 && b.shift != 0 && b.cols >= 256 && static_cast<int64_t>(cdiv(a.rows, 256)) * cdiv(b.rows, 256) > 128) {
+    const dim3 grid(static_cast<unsigned>(cdiv(a.rows, 256)) * cdiv(b.rows, 256));
+    if (a.e5m2)
+      hipLaunchKernelGGL((big8_kernel<true>), grid, dim3(512), 0, stream, b, a, b.cols, out);
+    else
+      hipLaunchKernelGGL((big8_kernel<false>), grid, dim3(512), 0, stream, b, a, b.cols, out);
+    return hipGetLastError();
+  }
   if (a.rows <= 32) return launch_ring8<128, 32, 64, 32, 4>(b, a, c_f32, out, stream);
   if (a.rows <= 64) return launch_ring8<128, 64, 64, 32, 3>(b, a, c_f32, out, stream);
-  return launch_ring8<128, 128, 64, 64, 3>(b, a, c_f32, out, stream);
+  return launch_ring8<128, 128, 64, 64, 2>(b, a, c_f32, out, stream);
 }
 
 }  // namespace ee

@@ -194,6 +194,28 @@ def test_product(m, n, k, ca, bra, brb, dtype):
     assert (got[m] == 7).all()
 
 
+@pytest.mark.parametrize("m,n,k,ca,spare", [
+    (1030, 9000, 300, "e4m3", 0), (1030, 9001, 512, "e5m2", 16), (2049, 4104, 256, "e4m3", 0), (300, 33001, 400, "e4m3", 32),
+    (257, 16800, 1033, "e5m2", 0), (4100, 2300, 392, "e4m3", 16),
+])
+def test_bf16_products_of_many_tiles(m, n, k, ca, spare):
+    """More 256 x 256 tiles than half of the CUs: ragged in every direction, two stages and more, sums that end inside a stage."""
+    say(f"case: scaled matmul big {m}x{n}x{k} {ca} spare {spare}")
+    assert -(-m // 256) * -(-n // 256) > 128 and k >= 256
+    a, sa, b, sb = operands(m, n, k, ca, 1, 128, m + n)
+    ref, bound = reference(a, sa, 1, b, sb, 128)
+    bound = bound + 7 * 2.0 ** -13 * group_maxima(Q.values(a, sa, 1), Q.values(b, sb, 128))
+    bound = bound + 2.0 ** -8 * (np.abs(ref) + bound)
+    da, db = Device.of(a, sa, 1, ca, spare), Device.of(b, sb, 128, "e4m3", spare)
+    c = torch.full((m + 1, n + spare), 7.0, dtype=torch.bfloat16, device="cuda")
+    for _ in range(2):
+        B.ee_scaled_matmul(da.c, db.c, c, B.EE_BF16, n + spare, 0, stream())
+    got = c.double().cpu().numpy()
+    err = np.abs(got[:m, :n] - ref)
+    assert (err <= bound).all(), (np.argmax(err - bound), err.max(), bound.min())
+    assert (got[m] == 7).all() and (got[:, n:] == 7).all()
+
+
 @pytest.mark.parametrize("m,n,k", [(3, 130, 300), (70, 333, 1000), (300, 600, 520)])
 def test_strides_accumulate_and_columns_past_the_last(m, n, k):
     say(f"case: scaled matmul strides {m}x{n}x{k}")
