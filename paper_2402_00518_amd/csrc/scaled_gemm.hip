@@ -34,15 +34,10 @@ namespace {
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 
-// 4 bytes a lane from base + off to LDS, lane l's at lds + 4 l (see load_lds16).
-__device__ __forceinline__ void load_lds4(const char *base, uint32_t off, uint32_t lds) {
-  const uint64_t b = reinterpret_cast<uint64_t>(base);
-  base = reinterpret_cast<const char *>(
-      static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b)))) |
-      static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(b >> 32)))) << 32);
+// 4 bytes a lane from the lane's address to LDS, lane l's at lds + 4 l (see load_lds16).
+__device__ __forceinline__ void load_lds4(const float *p, uint32_t lds) {
   lds = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(lds)));
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base)
-               : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
 }
 
 // E5: the columns' codes are e5m2.
@@ -84,44 +79,45 @@ __device__ __forceinline__ f32x4_t mfma_wide(const bf16x8_t (&a)[4], const bf16x
   return d;
 }
 
-// One operand of a stage of 128 values of K: ROWS rows of 128 bytes in LDS, 16-byte
-// chunk c of row r at c ^ ((r / 2) mod 8).  A lane's 32 bytes of a row are chunks g
-// and 4 + g (g = lane / 16); which values of K those are does not matter, as both
+// One operand of a stage of KW blocks of 128 values of K: for each block ROWS rows of 128 bytes
+// in LDS, 16-byte chunk c of row r at c ^ ((r / 2) mod 8).  A lane's 32 bytes of a row are
+// chunks g and 4 + g (g = lane / 16); which values of K those are does not matter, as both
 // operands take the same.
-template <int ROWS, int THREADS>
+template <int ROWS, int THREADS, int KW>
 struct Operand8 {
-  static constexpr int LOADS = ROWS * 8 / THREADS;
-  static constexpr int BYTES = ROWS * 128;
-  static_assert(LOADS * THREADS == ROWS * 8, "every thread loads the same number of chunks");
+  static constexpr int LOADS = KW * ROWS * 8 / THREADS;
+  static constexpr int BYTES = KW * ROWS * 128;
+  static_assert(LOADS * THREADS == KW * ROWS * 8, "every thread loads the same number of chunks");
   uint32_t off[LOADS];
-  int ch[LOADS];
+  int at[LOADS];  // bytes of the chunk from the stage's first
   const char *rd[2];
   const char *base;
 
-  __device__ __forceinline__ void init(const ScaledMat &m, int row0, int tid, int wrow, int lane, const char *lds) {
+  // kw: the block of the stage that the wave takes
+  __device__ __forceinline__ void init(const ScaledMat &m, int row0, int tid, int wrow, int kw, int lane, const char *lds) {
     base = reinterpret_cast<const char *>(m.data) + static_cast<int64_t>(row0) * m.ld;
     const uint32_t ld = static_cast<uint32_t>(m.ld);
     static_for<LOADS>([&](auto e) EE_ALWAYS_INLINE {
-      const int c = decltype(e)::value * THREADS + tid, lr = c >> 3;
-      ch[e] = (c & 7) ^ ((lr >> 1) & 7);
-      off[e] = static_cast<uint32_t>(min(row0 + lr, m.rows - 1) - row0) * ld + ch[e] * 16;
+      const int c = decltype(e)::value * THREADS + tid, lr = (c >> 3) % ROWS;
+      at[e] = (c / (ROWS * 8)) * 128 + ((c & 7) ^ ((lr >> 1) & 7)) * 16;
+      off[e] = static_cast<uint32_t>(min(row0 + lr, m.rows - 1) - row0) * ld;
     });
     const int r = lane & 15, x = (r >> 1) & 7;
     static_for<2>([&](auto h) EE_ALWAYS_INLINE {
-      rd[h] = lds + (wrow + r) * 128 + (((decltype(h)::value * 4 + (lane >> 4)) ^ x) << 4);
+      rd[h] = lds + (kw * ROWS + wrow + r) * 128 + (((decltype(h)::value * 4 + (lane >> 4)) ^ x) << 4);
     });
   }
   // Stage t, of which `left` bytes a row (a multiple of 16) are in the matrix: a
   // chunk past them re-reads the row's first one, and zero_tail clears it.
   __device__ __forceinline__ void load(int t, int left, uint32_t lds_wave) const {
-    const char *p = base + static_cast<int64_t>(t) * 128;
+    const char *p = base + static_cast<int64_t>(t) * (128 * KW);
     static_for<LOADS>([&](auto e) EE_ALWAYS_INLINE {
-      load_lds16(p, ch[e] * 16 < left ? off[e] : off[e] - ch[e] * 16, lds_wave + decltype(e)::value * THREADS * 16);
+      load_lds16(p, off[e] + (at[e] < left ? at[e] : 0), lds_wave + decltype(e)::value * THREADS * 16);
     });
   }
   __device__ __forceinline__ void zero_tail(int left, int tid, char *lds) const {
     static_for<LOADS>([&](auto e) EE_ALWAYS_INLINE {
-      if (ch[e] * 16 >= left)
+      if (at[e] >= left)
         *reinterpret_cast<u32x4_t *>(lds + (decltype(e)::value * THREADS + tid) * 16) = u32x4_t{0, 0, 0, 0};
     });
   }
@@ -192,52 +188,55 @@ __device__ __forceinline__ void store_row8(const StoreC &s, int row, int f, u32x
 __device__ __forceinline__ i32x8_t fragment(const bf16x8_t (&f)[2]) { return __builtin_bit_cast(i32x8_t, f); }
 
 // Ring of NS stages, the stage NS - 1 further on loaded while one is consumed, one
-// barrier a stage (as Ring of ring.h).  W: the rows operand, Z: the columns.  ROW1: W's
-// scales are one for each row, else one for each 128 (a wave's rows lie in one block).
-// E5: Z's codes are e5m2.  WIDE: C is fp32.
-template <int BM, int BN, int WM, int WN, int NS, bool ROW1, bool E5, bool WIDE>
-__global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void ring8_kernel(ScaledMat W, ScaledMat Z, int K, StoreC out) {
-  constexpr int WAVES_N = BN / WN, THREADS = BM / WM * WAVES_N * 64;
-  using TW = Operand8<BM, THREADS>;
-  using TZ = Operand8<BN, THREADS>;
-  constexpr int SL = (BM + BN + THREADS - 1) / THREADS;  // scale loads a thread and stage
+// barrier a stage (as Ring of ring.h).  W: the rows operand, Z: the columns.  KW waves share a
+// wave's WM x WN outputs: a stage is KW blocks of K, one for each, and their sums meet in LDS.
+// ROW1: W's scales are one for each row, else one for each 128 (a wave's rows lie in one
+// block).  E5: Z's codes are e5m2.  WIDE: C is fp32.
+template <int BM, int BN, int WM, int WN, int KW, int NS, bool ROW1, bool E5, bool WIDE>
+__global__ __launch_bounds__(BM / WM * (BN / WN) * KW * 64) void ring8_kernel(ScaledMat W, ScaledMat Z, int K, StoreC out) {
+  constexpr int WAVES_N = BN / WN, WAVES = BM / WM * WAVES_N, THREADS = WAVES * KW * 64;
+  using TW = Operand8<BM, THREADS, KW>;
+  using TZ = Operand8<BN, THREADS, KW>;
+  constexpr int SROWS = KW * (BM + BN);  // scales of a stage: W's rows and Z's, block by block
+  constexpr int SL = (SROWS + THREADS - 1) / THREADS;
   constexpr int S_OFF = TW::BYTES + TZ::BYTES, STAGE = S_OFF + SL * THREADS * 4;
   constexpr int LOADS = TW::LOADS + TZ::LOADS + SL;
+  constexpr int RED = KW > 1 ? KW * BM * BN * 4 : 0;
   static_assert((NS - 2) * LOADS <= 63, "loads in flight past the waited-for stage");
-  __shared__ __attribute__((aligned(128))) char smem[NS * STAGE];
+  __shared__ __attribute__((aligned(128))) char smem[NS * STAGE > RED ? NS * STAGE : RED];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int tiles_m = cdiv(W.rows, BM), tiles_n = cdiv(Z.rows, BN);
+  const int kw = wave / WAVES, ww = wave % WAVES;
   int tile_m, tile_n;
-  tile_of_block(blockIdx.x, gridDim.x, tiles_m, tiles_n, tile_m, tile_n);
+  tile_of_block(blockIdx.x, gridDim.x, cdiv(W.rows, BM), cdiv(Z.rows, BN), tile_m, tile_n);
   const int m0 = tile_m * BM, n0 = tile_n * BN;
-  const int wm = (wave / WAVES_N) * WM, wn = (wave % WAVES_N) * WN;
-  const int nk = cdiv(K, 128), bytes = (K + 15) & ~15;
+  const int wm = (ww / WAVES_N) * WM, wn = (ww % WAVES_N) * WN;
+  const int blocks = cdiv(K, 128), nk = cdiv(blocks, KW), bytes = (K + 15) & ~15;
   TW tw;
   TZ tz;
-  tw.init(W, m0, tid, wm, lane, smem);
-  tz.init(Z, n0, tid, wn, lane, smem + TW::BYTES);
-  // scale e of this thread: of W's row, or, past BM, of Z's (past those, the last again)
-  const char *sbase[SL];
-  uint32_t soff[SL];
-  int64_t sstep[SL];
+  tw.init(W, m0, tid, wm, kw, lane, smem);
+  tz.init(Z, n0, tid, wn, kw, lane, smem + TW::BYTES);
+  // Scale i of a stage: block i / (BM + BN), of W's row or, past BM, of Z's (past all, the
+  // last again).  A block of K past the last repeats its scale: its codes are zeros.
+  const float *sptr[SL];
+  int sblk[SL];
+  int64_t sld[SL];
   static_for<SL>([&](auto e) EE_ALWAYS_INLINE {
-    const int i = decltype(e)::value * THREADS + wave * 64;  // a wave's 64 scales come from one side
-    const bool w = i < BM;
-    const ScaledMat &m = w ? W : Z;
-    const int row = min((w ? m0 + i : n0 + i - BM) + lane, m.rows - 1);
-    sbase[e] = reinterpret_cast<const char *>(m.scale);
-    soff[e] = static_cast<uint32_t>(row >> m.shift) * 4;
-    sstep[e] = m.scale_ld * 4;
+    const int i = min(decltype(e)::value * THREADS + tid, SROWS - 1), r = i % (BM + BN);
+    const bool w = r < BM;
+    const int row = w ? min(m0 + r, W.rows - 1) >> W.shift : min(n0 + r - BM, Z.rows - 1) >> Z.shift;
+    sptr[e] = (w ? W.scale : Z.scale) + row;
+    sld[e] = w ? W.scale_ld : Z.scale_ld;
+    sblk[e] = i / (BM + BN);
   });
-  static_assert(BM % 64 == 0, "a wave's scales come from one side");
   const uint32_t lds0 =
       static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)smem));
   auto load = [&](int t, int buf) EE_ALWAYS_INLINE {
     const uint32_t l = lds0 + buf * STAGE + wave * 1024;
-    tw.load(t, bytes - t * 128, l);
-    tz.load(t, bytes - t * 128, l + TW::BYTES);
+    tw.load(t, bytes - t * (128 * KW), l);
+    tz.load(t, bytes - t * (128 * KW), l + TW::BYTES);
     static_for<SL>([&](auto e) EE_ALWAYS_INLINE {
-      load_lds4(sbase[e] + t * sstep[e], soff[e], lds0 + buf * STAGE + S_OFF + (decltype(e)::value * THREADS + wave * 64) * 4);
+      load_lds4(sptr[e] + min(t * KW + sblk[e], blocks - 1) * sld[e],
+                lds0 + buf * STAGE + S_OFF + (decltype(e)::value * THREADS + wave * 64) * 4);
     });
   };
   f32x4_t acc[WM / 16][WN / 16];
@@ -253,8 +252,8 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void ring8_kernel(ScaledM
     static_for<NS - 1>([&](auto l) EE_ALWAYS_INLINE {
       if (later == decltype(l)::value) wait_vm<decltype(l)::value * LOADS>();
     });
-    const int left = bytes - t * 128;
-    if (left < 128) {  // the last stage: each thread clears the chunks past K that it loaded itself
+    const int left = bytes - t * (128 * KW);
+    if (left < 128 * KW) {  // the last stage: each thread clears the chunks past K that it loaded itself
       tw.zero_tail(left, tid, smem + cur * STAGE);
       tz.zero_tail(left, tid, smem + cur * STAGE + TW::BYTES);
       wait_lgkm();
@@ -262,7 +261,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void ring8_kernel(ScaledM
     phase_barrier();
     if (t + NS - 1 < nk) load(t + NS - 1, cur == 0 ? NS - 1 : cur - 1);  // over stage t - 1, which every wave has read
     const int stage = cur * STAGE;
-    const float *sc = reinterpret_cast<const float *>(smem + stage + S_OFF);
+    const float *sc = reinterpret_cast<const float *>(smem + stage + S_OFF) + kw * (BM + BN);
     i32x8_t fw[WM / 16], fz[WN / 16];
     float zs[WN / 16];
     tz.template read<WN / 16>(stage, fz);
@@ -294,12 +293,32 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * 64) void ring8_kernel(ScaledM
     wait_lgkm();
     cur = cur == NS - 1 ? 0 : cur + 1;
   }
-  static_for<WM / 16>([&](auto i) EE_ALWAYS_INLINE {
-    static_for<WN / 16>([&](auto j) EE_ALWAYS_INLINE {
-      store_c<WIDE>(out, n0 + wn + decltype(j)::value * 16 + (lane & 15), m0 + wm + decltype(i)::value * 16 + (lane >> 4) * 4,
-              acc[i][j]);
+  auto store = [&](int i, int j, f32x4_t v) EE_ALWAYS_INLINE {  // 16 x 16 block of the tile
+    store_c<WIDE>(out, n0 + j * 16 + (lane & 15), m0 + i * 16 + (lane >> 4) * 4, v);
+  };
+  if constexpr (KW == 1) {
+    static_for<WM / 16>([&](auto i) EE_ALWAYS_INLINE {
+      static_for<WN / 16>([&](auto j) EE_ALWAYS_INLINE {
+        store(wm / 16 + decltype(i)::value, wn / 16 + decltype(j)::value, acc[i][j]);
+      });
     });
-  });
+  } else {
+    constexpr int ALL = (BM / 16) * (BN / 16);
+    f32x4_t *red = reinterpret_cast<f32x4_t *>(smem);  // [kw][16 x 16 block][lane]
+    __syncthreads();
+    static_for<WM / 16>([&](auto i) EE_ALWAYS_INLINE {
+      static_for<WN / 16>([&](auto j) EE_ALWAYS_INLINE {
+        const int b = (wm / 16 + decltype(i)::value) * (BN / 16) + wn / 16 + decltype(j)::value;
+        red[(kw * ALL + b) * 64 + lane] = acc[i][j];
+      });
+    });
+    __syncthreads();
+    for (int b = wave; b < ALL; b += WAVES * KW) {
+      f32x4_t v = red[b * 64 + lane];
+      static_for<KW - 1>([&](auto w) EE_ALWAYS_INLINE { v += red[((decltype(w)::value + 1) * ALL + b) * 64 + lane]; });
+      store(b / (BN / 16), b % (BN / 16), v);
+    }
+  }
 }
 
 // bf16 C, weights with 128 x 128 blocks: 256 x 256 tiles on 8 waves of 128 features x 64
@@ -327,12 +346,9 @@ __global__ __launch_bounds__(512, 1) void big8_kernel(ScaledMat W, ScaledMat Z, 
       static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char *)smem));
   const uint32_t lds_wave = lds0 + wave * 1024;
   const ScaledMat &side = wave < 4 ? W : Z;  // whose scales this wave loads
-  const char *sbase = reinterpret_cast<const char *>(side.scale);
-  const uint32_t soff =
-      static_cast<uint32_t>(min((wave < 4 ? m0 + tid : n0 + tid - 256), side.rows - 1) >> side.shift) * 4;
-  const int64_t sstep = side.scale_ld * 4;
+  const float *sptr = side.scale + (min((wave < 4 ? m0 + tid : n0 + tid - 256), side.rows - 1) >> side.shift);
   auto load_s = [&](int t, int u) EE_ALWAYS_INLINE {  // stage u's, to stage t's place
-    load_lds4(sbase + u * sstep, soff, lds0 + kBigStages + (t & 3) * kBigScales + wave * 256);
+    load_lds4(sptr + u * side.scale_ld, lds0 + kBigStages + (t & 3) * kBigScales + wave * 256);
   };
   auto load_a = [&](auto q, auto buf, int t) EE_ALWAYS_INLINE {
     ta.template load<decltype(q)::value>(min(t, nk - 1), 64, lds_wave + decltype(buf)::value * 65536);
@@ -486,29 +502,125 @@ __global__ __launch_bounds__(512, 1) void big8_kernel(ScaledMat W, ScaledMat Z, 
   });
 }
 
-template <int BM, int BN, int WM, int WN, int NS>
+// Few tokens, weights streamed once: a block has 16 RB features and up to 16 NB tokens, its
+// waves share K and read both operands straight into MFMA fragments, U blocks of K at a
+// time; their sums meet in LDS and each wave finishes some of the 16 x 16 blocks.
+template <int RB, int NB, int WAVES, int U, bool ROW1, bool E5, bool WIDE>
+__global__ __launch_bounds__(64 * WAVES) void skinny8_kernel(ScaledMat W, ScaledMat Z, int K, StoreC out) {
+  __shared__ f32x4_t red[WAVES][RB * NB][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m0 = blockIdx.x * 16 * RB, n0 = blockIdx.y * 16 * NB;
+  const int bytes = (K + 15) & ~15, nk = cdiv(bytes, 128);
+  const int k0 = wave * nk / WAVES, k1 = (wave + 1) * nk / WAVES, g = lane >> 4;
+  const uint8_t *wp[RB], *zp[NB];
+  const float *zsp[NB];
+  static_for<RB>([&](auto i) EE_ALWAYS_INLINE {
+    wp[i] = W.data + static_cast<int64_t>(min(m0 + decltype(i)::value * 16 + (lane & 15), W.rows - 1)) * W.ld + g * 16;
+  });
+  static_for<NB>([&](auto j) EE_ALWAYS_INLINE {
+    const int row = min(n0 + decltype(j)::value * 16 + (lane & 15), Z.rows - 1);
+    zp[j] = Z.data + static_cast<int64_t>(row) * Z.ld + g * 16;
+    zsp[j] = Z.scale + (row >> Z.shift);
+  });
+  f32x4_t acc[RB][NB];
+  static_for<RB>([&](auto i) EE_ALWAYS_INLINE {
+    static_for<NB>([&](auto j) EE_ALWAYS_INLINE { acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}; });
+  });
+  auto load = [&](const uint8_t *p, int k, int left) EE_ALWAYS_INLINE {
+    // chunks g and 4 + g of the row's 128 bytes; past the matrix: zeros, read from its row's first
+    const uint8_t *at = p + static_cast<int64_t>(k) * 128;
+    i32x4_t lo = *reinterpret_cast<const i32x4_t *>(g * 16 < left ? at : at - g * 16);
+    i32x4_t hi = *reinterpret_cast<const i32x4_t *>(64 + g * 16 < left ? at + 64 : at - g * 16);
+    if (left < 128) {
+      const i32x4_t zero = {0, 0, 0, 0};
+      if (g * 16 >= left) lo = zero;
+      if (64 + g * 16 >= left) hi = zero;
+    }
+    return i32x8_t(__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  // N blocks of K from k on, all loads ahead of the products
+  auto step = [&](auto n, int k, int left) EE_ALWAYS_INLINE {
+    constexpr int N = decltype(n)::value;
+    i32x8_t fw[N][RB], fz[N][NB];
+    float zs[N][NB];
+    f32x4_t ws[N][ROW1 ? RB : 1];
+    static_for<N>([&](auto q) EE_ALWAYS_INLINE {
+      constexpr int Q = decltype(q)::value;
+      const int l = Q == N - 1 ? left : 128;
+      static_for<RB>([&](auto i) EE_ALWAYS_INLINE { fw[Q][i] = load(wp[i], k + Q, l); });
+      static_for<NB>([&](auto j) EE_ALWAYS_INLINE { fz[Q][j] = load(zp[j], k + Q, l); });
+      static_for<NB>([&](auto j) EE_ALWAYS_INLINE { zs[Q][j] = zsp[j][(k + Q) * Z.scale_ld]; });
+      const float *s = W.scale + (k + Q) * W.scale_ld;
+      if constexpr (ROW1) {
+        static_for<RB>([&](auto i) EE_ALWAYS_INLINE {
+          const int r = m0 + decltype(i)::value * 16 + g * 4;
+          ws[Q][i] = f32x4_t{s[min(r, W.rows - 1)], s[min(r + 1, W.rows - 1)], s[min(r + 2, W.rows - 1)], s[min(r + 3, W.rows - 1)]};
+        });
+      } else {
+        const float v = s[m0 >> 7];  // (16 RB features lie in one block of 128)
+        ws[Q][0] = f32x4_t{v, v, v, v};
+      }
+    });
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<N>([&](auto q) EE_ALWAYS_INLINE {
+      constexpr int Q = decltype(q)::value;
+      bf16x8_t wz[WIDE ? NB : 1][4];
+      if constexpr (WIDE) static_for<NB>([&](auto j) EE_ALWAYS_INLINE { widen32<E5>(fz[Q][j], wz[j]); });
+      static_for<RB>([&](auto i) EE_ALWAYS_INLINE {
+        bf16x8_t ww[4];
+        if constexpr (WIDE) widen32<false>(fw[Q][i], ww);
+        static_for<NB>([&](auto j) EE_ALWAYS_INLINE {
+          f32x4_t d;
+          if constexpr (WIDE)
+            d = mfma_wide(ww, wz[j]);
+          else
+            d = mfma8<E5>(fw[Q][i], fz[Q][j]);
+          acc[i][j] += d * (ws[Q][ROW1 ? decltype(i)::value : 0] * zs[Q][j]);
+        });
+      });
+    });
+  };
+  const int whole = min(k1, bytes / 128);  // blocks of K that the matrix fills
+  int k = k0;
+  for (; k + U <= whole; k += U) step(std::integral_constant<int, U>{}, k, 128);
+  for (; k < k1; ++k) step(std::integral_constant<int, 1>{}, k, min(bytes - k * 128, 128));
+  static_for<RB>([&](auto i) EE_ALWAYS_INLINE {
+    static_for<NB>([&](auto j) EE_ALWAYS_INLINE { red[wave][decltype(i)::value * NB + decltype(j)::value][lane] = acc[i][j]; });
+  });
+  __syncthreads();
+  for (int b = wave; b < RB * NB; b += WAVES) {
+    f32x4_t v = red[0][b][lane];
+    static_for<WAVES - 1>([&](auto w) EE_ALWAYS_INLINE { v += red[decltype(w)::value + 1][b][lane]; });
+    store_c<WIDE>(out, n0 + (b % NB) * 16 + (lane & 15), m0 + (b / NB) * 16 + g * 4, v);
+  }
+}
+
+// f(ROW1, E5, WIDE) for the matrices and C's type.
+template <class F>
+hipError_t with_types(const ScaledMat &W, const ScaledMat &Z, bool f32, F &&f) {
+  auto by = [&](auto row1, auto e5) { return f32 ? f(row1, e5, std::true_type{}) : f(row1, e5, std::false_type{}); };
+  if (W.shift == 0) return Z.e5m2 ? by(std::true_type{}, std::true_type{}) : by(std::true_type{}, std::false_type{});
+  return Z.e5m2 ? by(std::false_type{}, std::true_type{}) : by(std::false_type{}, std::false_type{});
+}
+
+template <int RB, int NB, int WAVES, int U>
+hipError_t launch_skinny8(const ScaledMat &W, const ScaledMat &Z, bool f32, const StoreC &out, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>(cdiv(W.rows, 16 * RB)), static_cast<unsigned>(cdiv(Z.rows, 16 * NB)));
+  return with_types(W, Z, f32, [&](auto row1, auto e5, auto wide) {
+    hipLaunchKernelGGL((skinny8_kernel<RB, NB, WAVES, U, decltype(row1)::value, decltype(e5)::value, decltype(wide)::value>),
+                       grid, dim3(64 * WAVES), 0, stream, W, Z, W.cols, out);
+    return hipGetLastError();
+  });
+}
+
+template <int BM, int BN, int WM, int WN, int KW, int NS>
 hipError_t launch_ring8(const ScaledMat &W, const ScaledMat &Z, bool f32, const StoreC &out, hipStream_t stream) {
   const int64_t blocks = static_cast<int64_t>(cdiv(W.rows, BM)) * cdiv(Z.rows, BN);
-  const dim3 grid(static_cast<unsigned>(blocks)), block(BM / WM * (BN / WN) * 64);
-  auto go = [&](auto row1, auto e5, auto wide) {
-    hipLaunchKernelGGL((ring8_kernel<BM, BN, WM, WN, NS, decltype(row1)::value, decltype(e5)::value, decltype(wide)::value>),
-                       grid, block, 0, stream, W, Z, W.cols, out);
-  };
-  auto by = [&](auto row1, auto e5) {
-    if (f32)
-      go(row1, e5, std::true_type{});
-    else
-      go(row1, e5, std::false_type{});
-  };
-  if (W.shift == 0 && Z.e5m2)
-    by(std::true_type{}, std::true_type{});
-  else if (W.shift == 0)
-    by(std::true_type{}, std::false_type{});
-  else if (Z.e5m2)
-    by(std::false_type{}, std::true_type{});
-  else
-    by(std::false_type{}, std::false_type{});
-  return hipGetLastError();
+  return with_types(W, Z, f32, [&](auto row1, auto e5, auto wide) {
+    hipLaunchKernelGGL((ring8_kernel<BM, BN, WM, WN, KW, NS, decltype(row1)::value, decltype(e5)::value, decltype(wide)::value>),
+                       dim3(static_cast<unsigned>(blocks)), dim3(BM / WM * (BN / WN) * KW * 64), 0, stream, W, Z, W.cols, out);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace
@@ -526,9 +638,9 @@ hipError_t scaled_matmul(const ScaledMat &a, const ScaledMat &b, void *c, bool c
       hipLaunchKernelGGL((big8_kernel<false>), grid, dim3(512), 0, stream, b, a, b.cols, out);
     return hipGetLastError();
   }
-  if (a.rows <= 32) return launch_ring8<128, 32, 64, 32, 4>(b, a, c_f32, out, stream);
-  if (a.rows <= 64) return launch_ring8<128, 64, 64, 32, 3>(b, a, c_f32, out, stream);
-  return launch_ring8<128, 128, 64, 64, 2>(b, a, c_f32, out, stream);
+  if (a.rows <= 32) return launch_ring8<128, 32, 64, 32, 1, 4>(b, a, c_f32, out, stream);
+  if (a.rows <= 64) return launch_ring8<128, 64, 64, 32, 1, 3>(b, a, c_f32, out, stream);
+  return launch_ring8<128, 128, 64, 64, 1, 2>(b, a, c_f32, out, stream);
 }
 
 }  // namespace ee
