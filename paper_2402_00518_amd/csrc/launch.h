@@ -290,6 +290,10 @@ hipError_t launch_quantize(bool f32, const void *x, int64_t ldx, int rows, int c
 // they are) as e4m3 codes with a scale for each row and 128 values.  h: a multiple of 64.
 hipError_t launch_norm_quantize(bool x_f32, bool f32, const void *x, int n, int h, float eps, const void *gain, const void *bias,
                                 bool centre, const ScaledMat &q, hipStream_t stream, const float *extra = nullptr, int n_extra = 0);
+// The tile that scaled_matmul takes (row_scales: b has a scale for each row), as an index:
+// 0 256 x 256, 1 128 x 256, 2 128 x 128, 3 128 x 64, 4 64 x 128, 5 64 x 64, 6 64 x 32, 7 32 x 64, 8 32 x 32, 9 32
+// x 16 features by tokens, 10 to 12 direct loads (16 and 32 features on 4 waves, 16 on 8).
+int scaled_tile(bool c_f32, bool row_scales, int features, int tokens, int K);
 // C[i][j] (=|+=) sum over column blocks of the scales' product times the codes' dot
 // product: rows of a by rows of b, C [a.rows][ldc] in fp32 or bf16.
 hipError_t scaled_matmul(const ScaledMat &a, const ScaledMat &b, void *c, bool c_f32, int64_t ldc, int accumulate,

@@ -19,6 +19,8 @@
 // stores, and a weight's 128 x 128 blocks give one scale a wave and block.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
+
 #include "ee_device.h"
 #include "gemm.h"
 #include "launch.h"
@@ -595,10 +597,18 @@ __global__ __launch_bounds__(64 * WAVES) void skinny8_kernel(ScaledMat W, Scaled
   }
 }
 
-// f(ROW1, E5, WIDE) for the matrices and C's type.
-template <class F>
+// f(ROW1, E5, WIDE) for the matrices and C's type (of those that a tile is built for).
+template <bool F32, bool BF16, class F>
 hipError_t with_types(const ScaledMat &W, const ScaledMat &Z, bool f32, F &&f) {
-  auto by = [&](auto row1, auto e5) { return f32 ? f(row1, e5, std::true_type{}) : f(row1, e5, std::false_type{}); };
+  auto by = [&](auto row1, auto e5) {
+    if constexpr (F32) {
+      if (f32) return f(row1, e5, std::true_type{});
+    }
+    if constexpr (BF16) {
+      if (!f32) return f(row1, e5, std::false_type{});
+    }
+    return hipErrorInvalidValue;
+  };
   if (W.shift == 0) return Z.e5m2 ? by(std::true_type{}, std::true_type{}) : by(std::true_type{}, std::false_type{});
   return Z.e5m2 ? by(std::false_type{}, std::true_type{}) : by(std::false_type{}, std::false_type{});
 }
@@ -606,41 +616,109 @@ hipError_t with_types(const ScaledMat &W, const ScaledMat &Z, bool f32, F &&f) {
 template <int RB, int NB, int WAVES, int U>
 hipError_t launch_skinny8(const ScaledMat &W, const ScaledMat &Z, bool f32, const StoreC &out, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(cdiv(W.rows, 16 * RB)), static_cast<unsigned>(cdiv(Z.rows, 16 * NB)));
-  return with_types(W, Z, f32, [&](auto row1, auto e5, auto wide) {
+  return with_types<true, true>(W, Z, f32, [&](auto row1, auto e5, auto wide) {
     hipLaunchKernelGGL((skinny8_kernel<RB, NB, WAVES, U, decltype(row1)::value, decltype(e5)::value, decltype(wide)::value>),
                        grid, dim3(64 * WAVES), 0, stream, W, Z, W.cols, out);
     return hipGetLastError();
   });
 }
 
-template <int BM, int BN, int WM, int WN, int KW, int NS>
+template <int BM, int BN, int WM, int WN, int KW, int NS, bool F32 = true, bool BF16 = true>
 hipError_t launch_ring8(const ScaledMat &W, const ScaledMat &Z, bool f32, const StoreC &out, hipStream_t stream) {
   const int64_t blocks = static_cast<int64_t>(cdiv(W.rows, BM)) * cdiv(Z.rows, BN);
-  return with_types(W, Z, f32, [&](auto row1, auto e5, auto wide) {
+  return with_types<F32, BF16>(W, Z, f32, [&](auto row1, auto e5, auto wide) {
     hipLaunchKernelGGL((ring8_kernel<BM, BN, WM, WN, KW, NS, decltype(row1)::value, decltype(e5)::value, decltype(wide)::value>),
                        dim3(static_cast<unsigned>(blocks)), dim3(BM / WM * (BN / WN) * KW * 64), 0, stream, W, Z, W.cols, out);
     return hipGetLastError();
   });
 }
 
+// Which tile a product takes: the one of least time by a model, us with r rounds of T tiles
+// (features by tokens) over `slots` at a time, r1 rounds of one a CU, n tokens and K:
+//   rings and big8:  t0 + t1 r + t2 r K / 1000 + t3 T K / 1e5 + t4 r1 K / 1000
+//   direct loads:    t0 + t1 T / 1000 + t2 r K / 1000 + t3 T K / 1e5 + t4 T K n / 1.6e6
+// fitted to 36000 shapes (1 to 8192 tokens, 500 to 66000 features, K 320 to 16000), each
+// timed on every tile that could matter.  Over those shapes the choice is 2 to 3% slower in
+// the mean than the best of sixteen tiles, 16% in the worst twentieth.  What it weighs, us
+// of the best against the next (bf16 C unless fp32 is said):
+//   1 token: 32000 x 4096 direct 16 rows 23.7, 32 rows 24.9, ring 29.6; 8192 x 22016 16 rows
+//   and 8 waves 34.1, 4 waves 39.0;
+//   5120 x 13824: 16 tokens 32 x 16 shared by 8 waves 18.4, 32 x 32 20.0, direct 23.1; 48
+//   tokens 32 x 64 by 4 waves 27.9 (fp32 32.0), 64 x 64 by 2 35.0, unshared 48.0;
+//   13824 x 5120: 48 tokens 64 x 64 shared 19.4, unshared 22.6, 32 x 64 25.8; 200 tokens 128 x
+//   64 45.1, 128 x 128 48.9, 64 x 128 51.3;
+//   4096 tokens, 32000 x 4096: 256 x 256 470, 128 x 128 1156.
+struct Tile8 {
+  int bm, bn, slots;
+  float bf16[5], f32[5];  // t0 .. t4 by C's type (t1 < 0: none)
+};
+enum { kBig, k128x256, k128x128, k128x64, k64x128, k64x64, k64x32, k32x64, k32x32, k32x16, kDirect16, kDirect32, kDirect16by8, kTiles8 };
+constexpr Tile8 kTile8[kTiles8] = {
+    {256, 256, 256, {0.0f, 17.716f, 0.0f, 1.982f, 8.948f}, {0.0f, -1.0f}},
+    {128, 256, 256, {0.0f, -1.0f}, {0.0f, 11.229f, 11.484f, 2.039f, 0.0f}},
+    {128, 128, 512, {0.0f, 7.793f, 5.655f, 0.457f, 2.18f}, {0.0f, 8.767f, 3.162f, 0.841f, 5.249f}},
+    {128, 64, 512, {1.234f, 4.269f, 2.695f, 0.255f, 1.917f}, {0.949f, 5.15f, 1.486f, 0.284f, 3.935f}},
+    {64, 128, 256, {1.45f, 3.649f, 3.261f, 0.469f, 0.0f}, {1.279f, 4.625f, 4.623f, 0.441f, 0.0f}},
+    {64, 64, 256, {1.66f, 2.572f, 1.819f, 0.484f, 0.0f}, {1.327f, 3.333f, 0.0f, 0.358f, 2.425f}},
+    {64, 32, 512, {0.312f, 3.792f, 0.0f, 0.406f, 1.589f}, {0.0f, 4.264f, 0.0f, 0.367f, 1.943f}},
+    {32, 64, 256, {1.927f, 2.178f, 1.043f, 0.247f, 0.0f}, {1.608f, 2.541f, 1.596f, 0.225f, 0.0f}},
+    {32, 32, 256, {2.359f, 1.686f, 0.816f, 0.199f, 0.0f}, {2.101f, 1.958f, 1.029f, 0.165f, 0.0f}},
+    {32, 16, 256, {2.226f, 1.812f, 0.465f, 0.325f, 0.0f}, {1.919f, 2.141f, 0.637f, 0.28f, 0.0f}},
+    {16, 16, 2048, {4.039f, 0.0f, 0.312f, 0.229f, 0.126f}, {4.132f, 0.0f, 0.263f, 0.231f, 0.132f}},
+    {32, 16, 1024, {3.761f, 0.0f, 0.696f, 0.448f, 0.163f}, {3.774f, 0.0f, 0.792f, 0.456f, 0.169f}},
+    {16, 16, 1024, {4.154f, 0.249f, 0.145f, 0.249f, 0.121f}, {4.095f, 0.429f, 0.174f, 0.25f, 0.133f}},
+};
+
 }  // namespace
+
+int scaled_tile(bool c_f32, bool row_scales, int features, int tokens, int K) {
+  int best = -1;
+  double least = 0.0;
+  for (int i = 0; i < kTiles8; ++i) {
+    const Tile8 &t = kTile8[i];
+    const float *c = c_f32 ? t.f32 : t.bf16;
+    const bool direct = i >= kDirect16;
+    // (below 1024 values of K the big tile's loads are mostly the first stages' again)
+    if (c[1] < 0.0f || (i == kBig && (row_scales || K < 1024)) || (tokens > 16 ? direct : i < k32x32)) continue;
+    const double T = static_cast<double>(cdiv(features, t.bm)) * cdiv(tokens, t.bn), k = K * 1e-3;
+    const double r = std::ceil(T / t.slots), r1 = std::ceil(T / 256);
+    const double us = direct ? c[0] + c[1] * T * 1e-3 + c[2] * r * k + (c[3] + c[4] * tokens / 16.0) * T * k * 1e-2
+                             : c[0] + c[1] * r + c[2] * r * k + c[3] * T * k * 1e-2 + c[4] * r1 * k;
+    if (best < 0 || us < least) {
+      best = i;
+      least = us;
+    }
+  }
+  return best;
+}
 
 hipError_t scaled_matmul(const ScaledMat &a, const ScaledMat &b, void *c, bool c_f32, int64_t ldc, int accumulate,
                          hipStream_t stream) {
   if (a.rows <= 0 || b.rows <= 0) return hipSuccess;
   if (((a.cols + 15) & ~15) != ((b.cols + 15) & ~15) || b.e5m2) return hipErrorInvalidValue;
   const StoreC out{c, ldc, a.rows, b.rows, accumulate != 0, ldc % 4 == 0, ldc % 8 == 0};
-  if (!c_f32 && b.shift != 0 && b.cols >= 256 && static_cast<int64_t>(cdiv(a.rows, 256)) * cdiv(b.rows, 256) > 128) {
-    const dim3 grid(static_cast<unsigned>(cdiv(a.rows, 256)) * cdiv(b.rows, 256));
-    if (a.e5m2)
-      hipLaunchKernelGGL((big8_kernel<true>), grid, dim3(512), 0, stream, b, a, b.cols, out);
-    else
-      hipLaunchKernelGGL((big8_kernel<false>), grid, dim3(512), 0, stream, b, a, b.cols, out);
-    return hipGetLastError();
+  switch (scaled_tile(c_f32, b.shift == 0, b.rows, a.rows, b.cols)) {
+    case kBig: {
+      const dim3 grid(static_cast<unsigned>(cdiv(a.rows, 256)) * cdiv(b.rows, 256));
+      if (a.e5m2)
+        hipLaunchKernelGGL((big8_kernel<true>), grid, dim3(512), 0, stream, b, a, b.cols, out);
+      else
+        hipLaunchKernelGGL((big8_kernel<false>), grid, dim3(512), 0, stream, b, a, b.cols, out);
+      return hipGetLastError();
+    }
+    case k128x256: return launch_ring8<128, 256, 64, 64, 1, 2, true, false>(b, a, c_f32, out, stream);
+    case k128x128: return launch_ring8<128, 128, 64, 64, 1, 2>(b, a, c_f32, out, stream);
+    case k128x64: return launch_ring8<128, 64, 64, 32, 1, 3>(b, a, c_f32, out, stream);
+    case k64x128: return launch_ring8<64, 128, 32, 64, 2, 2>(b, a, c_f32, out, stream);
+    case k64x64: return launch_ring8<64, 64, 64, 32, 4, 2>(b, a, c_f32, out, stream);
+    case k64x32: return launch_ring8<64, 32, 32, 32, 2, 4>(b, a, c_f32, out, stream);
+    case k32x64: return launch_ring8<32, 64, 32, 32, 4, 3>(b, a, c_f32, out, stream);
+    case k32x32: return launch_ring8<32, 32, 32, 32, 4, 3>(b, a, c_f32, out, stream);
+    case k32x16: return launch_ring8<32, 16, 32, 16, 8, 3>(b, a, c_f32, out, stream);
+    case kDirect16: return launch_skinny8<1, 1, 4, 4>(b, a, c_f32, out, stream);
+    case kDirect32: return launch_skinny8<2, 1, 4, 4>(b, a, c_f32, out, stream);
+    default: return launch_skinny8<1, 1, 8, 4>(b, a, c_f32, out, stream);
   }
-  if (a.rows <= 32) return launch_ring8<128, 32, 64, 32, 1, 4>(b, a, c_f32, out, stream);
-  if (a.rows <= 64) return launch_ring8<128, 64, 64, 32, 1, 3>(b, a, c_f32, out, stream);
-  return launch_ring8<128, 128, 64, 64, 1, 2>(b, a, c_f32, out, stream);
 }
 
 }  // namespace ee

@@ -18,6 +18,8 @@ are off by less than 2^-13 of that largest one:
 the last for the rounding to bf16 (half a step).
 """
 
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -194,26 +196,54 @@ def test_product(m, n, k, ca, bra, brb, dtype):
     assert (got[m] == 7).all()
 
 
-@pytest.mark.parametrize("m,n,k,ca,spare", [
-    (1030, 9000, 300, "e4m3", 0), (1030, 9001, 512, "e5m2", 16), (2049, 4104, 256, "e4m3", 0), (300, 33001, 400, "e4m3", 32),
-    (257, 16800, 1033, "e5m2", 0), (4100, 2300, 392, "e4m3", 16),
-])
-def test_bf16_products_of_many_tiles(m, n, k, ca, spare):
-    """More 256 x 256 tiles than half of the CUs: ragged in every direction, two stages and more, sums that end inside a stage."""
-    say(f"case: scaled matmul big {m}x{n}x{k} {ca} spare {spare}")
-    assert -(-m // 256) * -(-n // 256) > 128 and k >= 256
-    a, sa, b, sb = operands(m, n, k, ca, 1, 128, m + n)
-    ref, bound = reference(a, sa, 1, b, sb, 128)
-    bound = bound + 7 * 2.0 ** -13 * group_maxima(Q.values(a, sa, 1), Q.values(b, sb, 128))
-    bound = bound + 2.0 ** -8 * (np.abs(ref) + bound)
-    da, db = Device.of(a, sa, 1, ca, spare), Device.of(b, sb, 128, "e4m3", spare)
-    c = torch.full((m + 1, n + spare), 7.0, dtype=torch.bfloat16, device="cuda")
+def tile_of(f32, row_scales, n, m, k):
+    """The tile that the library's rule gives a product (an index, see launch.h)."""
+    f = ctypes.CDLL(B.LIB_PATH)["_ZN2ee11scaled_tileEbbiii"]
+    f.restype, f.argtypes = ctypes.c_int, (ctypes.c_bool,) * 2 + (ctypes.c_int,) * 3
+    return f(f32, row_scales, n, m, k)
+
+
+def check_product(m, n, k, ca, brb, dtype, spare=0):
+    a, sa, b, sb = operands(m, n, k, ca, 1, brb, m + n)
+    va, vb = (torch.from_numpy(v).cuda() for v in (Q.values(a, sa, 1), Q.values(b, sb, brb)))
+    ref, bound = va @ vb.t(), (129 + sa.shape[0]) * 2.0 ** -23 * (va.abs() @ vb.abs().t())
+    if dtype == "bf16":
+        bound = bound + 7 * 2.0 ** -13 * torch.from_numpy(group_maxima(va.cpu().numpy(), vb.cpu().numpy())).cuda()
+        bound = bound + 2.0 ** -8 * (ref.abs() + bound)
+    da, db = Device.of(a, sa, 1, ca, spare), Device.of(b, sb, brb, "e4m3", spare)
+    c = torch.full((m + 1, n + spare), 7.0, dtype=DTYPES[dtype][1], device="cuda")
     for _ in range(2):
-        B.ee_scaled_matmul(da.c, db.c, c, B.EE_BF16, n + spare, 0, stream())
-    got = c.double().cpu().numpy()
-    err = np.abs(got[:m, :n] - ref)
-    assert (err <= bound).all(), (np.argmax(err - bound), err.max(), bound.min())
-    assert (got[m] == 7).all() and (got[:, n:] == 7).all()
+        B.ee_scaled_matmul(da.c, db.c, c, DTYPES[dtype][0], n + spare, 0, stream())
+    err = (c[:m, :n].double() - ref).abs()
+    assert bool((err <= bound).all()), (float(err.max()), float(bound.min()), int((err > bound).sum()))
+    assert bool((c[m] == 7).all()) and bool((c[:, n:] == 7).all())
+
+
+@pytest.mark.parametrize("m,n,k,ca,spare", [
+    (1030, 9000, 1100, "e4m3", 0), (1030, 9001, 1536, "e5m2", 16), (2049, 6104, 1024, "e4m3", 0), (900, 33001, 1040, "e4m3", 32),
+    (520, 16800, 1033, "e5m2", 0), (4100, 2300, 1208, "e4m3", 16),
+])
+def test_bf16_products_of_large_tiles(m, n, k, ca, spare):
+    """The 256 x 256 tile: ragged in every direction, even and odd numbers of stages, sums that end inside a stage."""
+    say(f"case: scaled matmul big {m}x{n}x{k} {ca} spare {spare}")
+    assert tile_of(False, False, n, m, k) == 0
+    check_product(m, n, k, ca, 128, "bf16", spare)
+
+
+# (tile, rows of a, rows of b, depth), for either type of C
+TILES = [(2, 262, 13273, 47), (3, 133, 8379, 175), (3, 140, 8379, 513), (4, 834, 1161, 300), (6, 19, 8577, 320), (7, 35, 4207, 200),
+         (7, 64, 5001, 2064), (8, 70, 1500, 1500), (8, 200, 1001, 500), (9, 17, 33, 32), (9, 12, 4001, 4100), (10, 3, 40001, 1100),
+         (10, 9, 12001, 2048), (11, 1, 32, 32), (11, 14, 20001, 500), (12, 1, 33, 723), (12, 5, 700, 3000)]
+TILES_F32 = [(1, 131, 23217, 1675), (1, 1147, 4037, 6348), (5, 241, 4003, 851)]
+TILES_BF16 = [(5, 170, 4621, 637), (5, 36, 8359, 80)]
+
+
+@pytest.mark.parametrize("ca,brb", [("e4m3", 128), ("e5m2", 1)])
+@pytest.mark.parametrize("dtype,tile,m,n,k", [("f32", *t) for t in TILES + TILES_F32] + [("bf16", *t) for t in TILES + TILES_BF16])
+def test_every_tile(dtype, tile, m, n, k, ca, brb):
+    say(f"case: scaled matmul tile {tile} {m}x{n}x{k} {ca} {brb} {dtype}")
+    assert tile_of(dtype == "f32", brb == 1, n, m, k) == tile
+    check_product(m, n, k, ca, brb, dtype)
 
 
 @pytest.mark.parametrize("m,n,k", [(3, 130, 300), (70, 333, 1000), (300, 600, 520)])
