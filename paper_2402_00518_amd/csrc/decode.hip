@@ -293,6 +293,37 @@ struct DecStoreLogits {
     int64_t ld;
     bool f32, vec;
   };
+  // Rows that are not aligned for wider stores: a wave's 64 vocabulary ids of NT tokens through
+  // its own LDS (256 bytes a token, 16-byte chunk c of token t at c ^ (t mod 16)), then 64
+  // consecutive logits of one token a store instead of pieces of 32 (V 32003, 200 tokens: 89
+  // -> 85 us).
+  template <int NT>
+  __device__ __forceinline__ static void apply_rows(const Params &p, const f32x16_t (&blk)[2][NT / 32], int r0, int j0,
+                                                    int lane, int R, int B, char *lds) {
+    static_for<2>([&](auto i) EE_ALWAYS_INLINE {
+      static_for<NT / 32>([&](auto j) EE_ALWAYS_INLINE {
+        constexpr int I = decltype(i)::value, J = decltype(j)::value;
+        static_for<4>([&](auto q) EE_ALWAYS_INLINE {
+          constexpr int Q = decltype(q)::value;
+          const int c = dec_row(32 * I, lane, 4 * Q) >> 2, t = 32 * J + (lane & 31);
+          *reinterpret_cast<f32x4_t *>(lds + t * 256 + ((c ^ (t & 15)) << 4)) =
+              f32x4_t{blk[I][J][4 * Q], blk[I][J][4 * Q + 1], blk[I][J][4 * Q + 2], blk[I][J][4 * Q + 3]};
+        });
+      });
+    });
+    wait_lgkm();
+    const int r = r0 + lane;
+    for (int t = 0; t < NT && j0 + t < B; ++t) {
+      const float v = *reinterpret_cast<const float *>(lds + t * 256 + (((lane >> 2) ^ (t & 15)) << 4) + (lane & 3) * 4);
+      const int64_t o = static_cast<int64_t>(j0 + t) * p.ld + r;
+      if (r < R) {
+        if (p.f32)
+          static_cast<float *>(p.out)[o] = v;
+        else
+          static_cast<bf16_t *>(p.out)[o] = f32_to_bf16(v);
+      }
+    }
+  }
   __device__ __forceinline__ static void apply(const Params &p, const f32x16_t &acc, int r0, int j0, int lane, int R,
                                                int B) {
     for_rows4(acc, r0, j0, lane, R, B, [&](int row0, int j, f32x4_t c) EE_ALWAYS_INLINE {
@@ -459,6 +490,13 @@ __global__ __launch_bounds__(BM / 64 * (BN / WN) * 64) void ring_kernel(Operand 
   f32x16_t blk[2][WN / 32];
   to_blocks32<2, WN / 32>(acc, blk);
   const int r0 = tile * BM + (wave / Rg::WAVES_N) * 64, t0 = j0 + (wave % Rg::WAVES_N) * WN;
+  if constexpr (std::is_same<Epi, DecStoreLogits>::value) {
+    static_assert(BM / 64 * (BN / WN) * WN * 256 <= NS * Rg::STAGE_BYTES, "room for every wave's logits");
+    if (!ep.vec) {  // (every wave has read the last stage, see Ring)
+      Epi::template apply_rows<WN>(ep, blk, r0, t0, lane, R, B, smem + wave * (WN * 256));
+      return;
+    }
+  }
   static_for<WN / 32>([&](auto j) EE_ALWAYS_INLINE {
     constexpr int J = decltype(j)::value;
     if constexpr (PAIR) {
@@ -529,6 +567,14 @@ hipError_t launch_ring(Operand W, int R, Operand Z, int B, int K, int splits, co
       if (blocks > 256) return launch_ring_cfg<Epi, 128, 128, 64, 2, 1, PAIR, 8>(W, R, Z, B, K, splits, ep, stream);
       return launch_ring_cfg<Epi, 128, 128, 64, 4, 1, PAIR, 8>(W, R, Z, B, K, splits, ep, stream);
     }
+  }
+  if constexpr (std::is_same<Epi, DecStoreLogits>::value) {
+    // Past 128 tokens groups of 256 that they fill more than half, so that W is staged once
+    // for all of them (7B, 200 tokens 88 -> 82 us, V 64000 172 -> 154; V 8000, 63 blocks, 55 -> 60;
+    // 300 tokens 140 -> 150).
+    const int64_t wide = static_cast<int64_t>((R + 127) / 128) * ((B + 255) / 256);
+    if (B > 128 && (B + 255) % 256 >= 128 && wide > 128)
+      return launch_ring_cfg<Epi, 128, 256, 64, 3, 1, PAIR>(W, R, Z, B, K, splits, ep, stream);
   }
   if (B <= 32) {
     if (camp) return launch_ring_cfg<Epi, 128, 32, 32, 4, 8, PAIR>(W, R, Z, B, K, splits, ep, stream);
