@@ -767,13 +767,34 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
       }
     }
     if (!by_count && bin < kBins - 1) {
-      // the bin's tokens, and on the way the mass that each wave has above it
+      // The bin's tokens, and on the way the mass that each wave has above it: its logits
+      // gather in a queue (where the sorted list comes later) and are taken 64 at a time, as
+      // few lanes have one (all lanes at every step: 60 us for 128000 tokens, so 30).
+      float *queue = reinterpret_cast<float *>(sh.sorted) + wave * (kSorted / W);
+      int queued = 0;
       len = make_list(false, [&](float x) EE_ALWAYS_INLINE {
-        if (!(x > -INFINITY)) return false;
-        const int b = bin_of(x);
-        if (b < bin && !again) above_bin += mass_of(x);
+        const int b = x > -INFINITY ? bin_of(x) : kBins;
+        const bool above = b < bin && !again;
+        const uint64_t mask = __ballot(above);
+        if (mask != 0) {
+          if (above)
+            queue[queued + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(mask >> 32),
+                                                     __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(mask), 0))] = x;
+          queued += __builtin_popcountll(mask);
+          if (queued >= 64) {
+            sync(Wave{});
+            const float v = queue[lane], rest = queue[64 + lane];
+            above_bin += mass_of(v);
+            sync(Wave{});
+            queued -= 64;
+            if (lane < queued) queue[lane] = rest;
+          }
+        }
         return b == bin;
       });
+      sync(Wave{});
+      if (lane < queued) above_bin += mass_of(queue[lane]);
+      __syncthreads();  // (the queues are overwritten next)
       in_bin = len <= min(kList, kSorted);
     }
     if (in_bin) {
