@@ -9,9 +9,10 @@
 // whole.  Masses and their sums are 64 bits wide: a sum of 32 over a vocabulary
 // would move its borders by more than the distance of neighbouring random numbers.
 //
-// One block of 16 waves a row.  Each wave holds a range of consecutive ids, so that
-// everything in the order of ids is a prefix over waves, then inside one.
-//   1. maximum;
+// One block a row, of 16 waves (8 for more than 256 rows that LDS does not hold, two blocks a
+// CU).  Each wave holds a range of consecutive ids, so that everything in the order of ids is
+// a prefix over waves, then inside one.
+//   1. maximum (the row goes into LDS on the way, if it fits);
 //   2. sum of masses, and in LDS a histogram over (max - x) / T in 2047 bins of
 //      1/64 and one for the rest: of counts for top-k, else of masses for top-p.
 //      (Masses as multiples of 2^-43, so that the order of the atomics does not show.)
@@ -21,7 +22,16 @@
 // Where the list would not fit, top-p alone lists the cut's bin only and walks the
 // row once more; what is left (a cut in the last bin, thousands of equal logits)
 // finds the cut by the digits of the logits' bits, three passes over the row.
+// Of up to 64 long rows that LDS does not hold, several blocks a row take steps 1 and 2.
+//
+// What bounds it: not the bytes.  A row's block walks its ids two to five times with some 45
+// cycles of a SIMD for 64 exponentials and their histogram entries, and between the walks
+// stand scans, a sort and about thirty barriers: 18 to 24 us for one row of 32000, where
+// reading it takes well under one.  512 rows of 128000 fp32 logits (262 MB, a pass over which
+// takes 46 us) with top-p 0.95: 231 us.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
 
 #include "ee_device.h"
 #include "launch.h"
@@ -241,18 +251,196 @@ struct Row {
   }
 };
 
-// W: waves of the block.
+// What a row's parameters ask for.
+struct RowPlan {
+  float temp, top_p, min_p, u;
+  int top_k;
+  bool valid, greedy, by_count, by_mass, cut, want_conf, same, need_z, need_z1;
+  double c1, ct;   // 64 log2(e), and that over the temperature
+  double least, p; // min-p and top-p
+  float bscale;
+
+  __device__ __forceinline__ RowPlan(const SampleArgs &a, int n) {
+    temp = a.temperature != nullptr ? a.temperature[n] : 1.0f;
+    top_k = a.top_k != nullptr ? a.top_k[n] : 0;
+    top_p = a.top_p != nullptr ? a.top_p[n] : 1.0f;
+    min_p = a.min_p != nullptr ? a.min_p[n] : 0.0f;
+    u = a.uniform[n];
+    valid = temp == temp && top_p == top_p && min_p == min_p && u == u;
+    greedy = !(temp > 0.0f);
+    by_count = !greedy && top_k > 0 && top_k < a.vocab;
+    by_mass = !greedy && top_p < 1.0f;
+    cut = by_count || by_mass;
+    want_conf = a.confidence != nullptr || a.exit_flag != nullptr;
+    // (an infinite temperature still sends -infinity to mass 0)
+    c1 = 64.0 / kLn2;
+    ct = greedy ? c1 : fmax(c1 / static_cast<double>(temp), 1e-300);
+    same = ct == c1;  // one mass serves both
+    least = min_p > 0.0f ? (min_p < 1.0f ? static_cast<double>(min_p) : 1.0) : 0.0;
+    p = top_p > 0.0f ? static_cast<double>(top_p) : 0.0;
+    need_z = (by_mass && !by_count) || (want_conf && same) || (!cut && !greedy && least == 0.0);
+    need_z1 = want_conf && !same;
+    bscale = static_cast<float>(kBinsPerUnit / (greedy ? 1.0 : static_cast<double>(temp)));
+  }
+  __device__ __forceinline__ int bin_of(float x, float mx) const {  // monotone in x
+    const float b = (mx - x) * bscale;
+    return b < static_cast<float>(kBins - 1) ? static_cast<int>(b) : kBins - 1;
+  }
+};
+
+// Sums of masses at both temperatures over the wave's share of the row, and the histogram.
+template <class R>
+__device__ __forceinline__ void sum_masses(const R &row, const RowPlan &plan, float mx, const double *table,
+                                           unsigned long long *hist, double &z, double &z1) {
+  const double dmx = mx;
+  auto pass = [&](auto with_z, auto with_z1, auto with_hist) EE_ALWAYS_INLINE {
+    row.each([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const double d = static_cast<double>(x[e]) - dmx;
+        double m = 0.0;
+        if constexpr (decltype(with_z)::value) {
+          // (exact zeros where the sums are used to find the token)
+          m = pow2_neg<!decltype(with_hist)::value>(d * plan.ct, table);
+          z += m;
+        }
+        if constexpr (decltype(with_z1)::value) z1 += pow2_neg<false>(d * plan.c1, table);
+        if constexpr (decltype(with_hist)::value) {
+          const int b = plan.bin_of(x[e], mx);
+          if (b < kBins - 1) atomicAdd(&hist[b], plan.by_count ? 1ull : units_of(m));
+        }
+      }
+    });
+  };
+  with_flag(plan.need_z, [&](auto f) EE_ALWAYS_INLINE {
+    with_flag(plan.need_z1, [&](auto g) EE_ALWAYS_INLINE { with_flag(plan.cut, [&](auto h) EE_ALWAYS_INLINE { pass(f, g, h); }); });
+  });
+}
+
+// Few rows leave most CUs idle while one block of each walks a long row: the maximum and the
+// sums with the histogram are then taken by `splits` blocks a row, in two launches ahead.
+struct Part {
+  float max;
+  int bad;
+  double z, z1;
+};
+constexpr int kPartWaves = 4;
+
+__device__ __forceinline__ int first_of_part(int vocab, int split, int splits) {  // (whole steps of 256 ids)
+  return static_cast<int>(static_cast<int64_t>((vocab + 255) / 256) * split / splits) * 256;
+}
+
+template <typename R>
+__device__ __forceinline__ void share_part(R &row, const SampleArgs &a, int split, int splits, int wave) {
+  const int from = first_of_part(a.vocab, split, splits), mine = (first_of_part(a.vocab, split + 1, splits) - from) / 256;
+  row.first = min(from + mine * wave / kPartWaves * 256, a.vocab);
+  row.last = min(from + mine * (wave + 1) / kPartWaves * 256, a.vocab);
+}
+
+template <typename T>
+__device__ __forceinline__ Row<T, false> global_row(const SampleArgs &a, int n, int lane) {
+  Row<T, false> row;
+  row.p = static_cast<const T *>(a.logits) + n * a.ld;
+  row.allowed = a.allowed != nullptr ? a.allowed + n * a.allowed_ld : nullptr;
+  row.cache = nullptr;
+  row.vocab = a.vocab;
+  row.vec = a.ld % 4 == 0;
+  row.lane = lane;
+  return row;
+}
+
+template <typename T>
+__global__ __launch_bounds__(64 * kPartWaves) void part_max_kernel(SampleArgs a, Part *parts) {
+  __shared__ float maxes[kPartWaves];
+  __shared__ int bads[kPartWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = blockIdx.y;
+  Row<T, false> row = global_row<T>(a, n, lane);
+  share_part(row, a, blockIdx.x, gridDim.x, wave);
+  float mx = -INFINITY;
+  bool bad = false;
+  row.each([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      mx = fmaxf(mx, x[e]);
+      bad |= x[e] != x[e];
+    }
+  });
+  mx = warp_max(mx);
+  bad = __any(bad);
+  if (lane == 0) {
+    maxes[wave] = mx;
+    bads[wave] = bad;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kPartWaves; ++w) {
+      mx = fmaxf(mx, maxes[w]);
+      bad |= bads[w] != 0;
+    }
+    Part &p = parts[n * gridDim.x + blockIdx.x];
+    p.max = mx;
+    p.bad = bad;
+  }
+}
+
+// The row's maximum, and whether it has a NaN, from its parts.
+__device__ __forceinline__ float max_of_parts(const Part *parts, int splits, bool &bad) {
+  float mx = -INFINITY;
+  for (int i = 0; i < splits; ++i) {
+    mx = fmaxf(mx, parts[i].max);
+    bad |= parts[i].bad != 0;
+  }
+  return mx;
+}
+
+template <typename T>
+__global__ __launch_bounds__(64 * kPartWaves) void part_sum_kernel(SampleArgs a, Part *parts, unsigned long long *hists) {
+  __shared__ unsigned long long hist[kBins];
+  __shared__ double table[64];
+  __shared__ double sums[2][kPartWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.y;
+  const int splits = gridDim.x, at = n * splits + blockIdx.x;
+  const RowPlan plan(a, n);
+  bool bad = !plan.valid;
+  const float mx = max_of_parts(parts + n * splits, splits, bad);
+  if (bad || mx == INFINITY || mx == -INFINITY || !(plan.need_z || plan.need_z1 || plan.cut)) return;
+  for (int i = tid; i < kBins; i += 64 * kPartWaves) hist[i] = 0;
+  if (tid < 64) table[tid] = kPow2.v[tid];
+  __syncthreads();
+  Row<T, false> row = global_row<T>(a, n, lane);
+  share_part(row, a, blockIdx.x, splits, wave);
+  double z = 0.0, z1 = 0.0;
+  sum_masses(row, plan, mx, table, hist, z, z1);
+  z = wave_sum(z);
+  z1 = wave_sum(z1);
+  if (lane == 0) {
+    sums[0][wave] = z;
+    sums[1][wave] = z1;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < kPartWaves; ++w) {
+      z += sums[0][w];
+      z1 += sums[1][w];
+    }
+    parts[at].z = z;
+    parts[at].z1 = z1;
+  }
+  if (plan.cut)
+    for (int i = tid; i < kBins; i += 64 * kPartWaves) hists[static_cast<int64_t>(at) * kBins + i] = hist[i];
+}
+
+// W: waves of the block.  splits > 0: steps 1 and 2 have been taken by the kernels above.
 template <typename T, bool CACHED, int W>
-__global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
+__global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a, const Part *parts, const unsigned long long *hists,
+                                                           int splits) {
   constexpr int kThreads = 64 * W, kList = list_of(CACHED);
   extern __shared__ __attribute__((aligned(16))) char smem[];
   auto &sh = *reinterpret_cast<Shared<kList> *>(smem);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.x;
-  const float temp = a.temperature != nullptr ? a.temperature[n] : 1.0f;
-  const int top_k = a.top_k != nullptr ? a.top_k[n] : 0;
-  const float top_p = a.top_p != nullptr ? a.top_p[n] : 1.0f;
-  const float min_p = a.min_p != nullptr ? a.min_p[n] : 0.0f;
-  const float u = a.uniform[n];
+  const RowPlan plan(a, n);
+  const int top_k = plan.top_k;
+  const float u = plan.u;
   Row<T, CACHED> row;
   row.cache = reinterpret_cast<typename Quad<T>::type *>(smem + shared_bytes(CACHED));
   row.p = static_cast<const T *>(a.logits) + n * a.ld;
@@ -283,18 +471,34 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
 
   // 1. the maximum, and whether the row has a distribution at all
   float mx = -INFINITY;
-  bool bad = temp != temp || top_p != top_p || min_p != min_p || u != u;
-  for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;  // (closed by the barrier below, as is the table)
-  if (tid < 64) sh.table[tid] = kPow2.v[tid];
-  row.template each<true>([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      mx = fmaxf(mx, x[e]);
-      bad |= x[e] != x[e];
+  bool bad = !plan.valid;
+  if (splits > 0) {
+    parts += n * splits;
+    hists += static_cast<int64_t>(n) * splits * kBins;
+    mx = max_of_parts(parts, splits, bad);
+    if (plan.cut) {
+      for (int i = tid; i < kBins; i += kThreads) {
+        unsigned long long h = 0;
+        if (!bad && mx < INFINITY && mx > -INFINITY)
+          for (int q = 0; q < splits; ++q) h += hists[static_cast<int64_t>(q) * kBins + i];
+        sh.hist[i] = h;
+      }
     }
-  });
-  mx = warp_max(mx);
-  bad = __any(bad);
+  } else {
+    for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;  // (closed by the barrier below, as is the table)
+  }
+  if (tid < 64) sh.table[tid] = kPow2.v[tid];
+  if (splits == 0) {
+    row.template each<true>([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        mx = fmaxf(mx, x[e]);
+        bad |= x[e] != x[e];
+      }
+    });
+    mx = warp_max(mx);
+    bad = __any(bad);
+  }
   if (lane == 0) {
     sh.part[0][wave] = mx;
     sh.ipart[0][wave] = bad;
@@ -317,53 +521,28 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
     }
     return;
   }
-  const bool greedy = !(temp > 0.0f);
-  // (an infinite temperature still sends -infinity to mass 0)
-  const double dmx = mx, c1 = 64.0 / kLn2, ct = greedy ? c1 : fmax(c1 / static_cast<double>(temp), 1e-300);
-  auto mass_of = [&](float x) EE_ALWAYS_INLINE { return pow2_neg((static_cast<double>(x) - dmx) * ct, sh.table); };
-  const bool want_conf = a.confidence != nullptr || a.exit_flag != nullptr;
-  const bool by_count = !greedy && top_k > 0 && top_k < a.vocab, by_mass = !greedy && top_p < 1.0f;
-  const bool cut = by_count || by_mass;
-  const bool same = ct == c1;  // one mass serves both
-  const double least = min_p > 0.0f ? (min_p < 1.0f ? static_cast<double>(min_p) : 1.0) : 0.0;
-  const double p = top_p > 0.0f ? static_cast<double>(top_p) : 0.0;
+  const bool by_count = plan.by_count, by_mass = plan.by_mass, cut = plan.cut;
+  const double dmx = mx, least = plan.least, p = plan.p;
+  const float bscale = plan.bscale;
+  auto mass_of = [&](float x) EE_ALWAYS_INLINE { return pow2_neg((static_cast<double>(x) - dmx) * plan.ct, sh.table); };
+  auto bin_of = [&](float x) EE_ALWAYS_INLINE { return plan.bin_of(x, mx); };
 
   // 2. sums of masses; the histogram
-  const float bscale = static_cast<float>(kBinsPerUnit / (greedy ? 1.0 : static_cast<double>(temp)));
-  auto bin_of = [&](float x) EE_ALWAYS_INLINE {  // monotone in x
-    const float b = (mx - x) * bscale;
-    return b < static_cast<float>(kBins - 1) ? static_cast<int>(b) : kBins - 1;
-  };
   double z = 0.0, z1 = 0.0;
-  const bool need_z = (by_mass && !by_count) || (want_conf && same) || (!cut && !greedy && least == 0.0);
-  const bool need_z1 = want_conf && !same;
-  if (need_z || need_z1 || cut) {
-    auto pass = [&](auto with_z, auto with_z1, auto with_hist) EE_ALWAYS_INLINE {
-      row.each([&](int, const float (&x)[4]) EE_ALWAYS_INLINE {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const double d = static_cast<double>(x[e]) - dmx;
-          double m = 0.0;
-          if constexpr (decltype(with_z)::value) {
-            m = pow2_neg<!decltype(with_hist)::value>(d * ct, sh.table);  // (exact zeros where step 4 may use the sums)
-            z += m;
-          }
-          if constexpr (decltype(with_z1)::value) z1 += pow2_neg<false>(d * c1, sh.table);
-          if constexpr (decltype(with_hist)::value) {
-            const int b = bin_of(x[e]);
-            if (b < kBins - 1) atomicAdd(&sh.hist[b], by_count ? 1ull : units_of(m));
-          }
-        }
-      });
-    };
-    with_flag(need_z, [&](auto f) EE_ALWAYS_INLINE {
-      with_flag(need_z1, [&](auto g) EE_ALWAYS_INLINE { with_flag(cut, [&](auto h) EE_ALWAYS_INLINE { pass(f, g, h); }); });
-    });
+  if (splits > 0) {
+    if (plan.need_z || plan.need_z1 || cut) {
+      for (int q = 0; q < splits; ++q) {
+        z += parts[q].z;
+        z1 += parts[q].z1;
+      }
+    }
+  } else if (plan.need_z || plan.need_z1 || cut) {
+    sum_masses(row, plan, mx, sh.table, sh.hist, z, z1);
     z = block_sum(z);  // (its barrier also closes the histogram)
-    if (need_z1) z1 = block_sum(z1);
+    if (plan.need_z1) z1 = block_sum(z1);
   }
-  if (want_conf && tid == 0) {
-    const float conf = static_cast<float>(1.0 / (same ? z : z1));
+  if (plan.want_conf && tid == 0) {
+    const float conf = static_cast<float>(1.0 / (plan.same ? z : z1));
     if (a.confidence != nullptr) a.confidence[n] = conf;
     if (a.exit_flag != nullptr) a.exit_flag[n] = conf > a.threshold ? 1 : 0;
   }
@@ -372,7 +551,7 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
     a.token[n] = token;
     if (a.prob != nullptr) a.prob[n] = static_cast<float>(prob);
   };
-  if (greedy) {
+  if (plan.greedy) {
     int at = 0x7FFFFFFF;
     row.each([&](int id, const float (&x)[4]) EE_ALWAYS_INLINE {
 #pragma unroll
@@ -732,7 +911,22 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
     // moved down past what its rounding may hide (a few tokens more do no harm).
     const float edge = (mx - static_cast<float>(bin + 1) / bscale), from = edge - 1e-5f * (fabsf(edge) + fabsf(mx));
     const bool all = bin == kBins - 1 || !(from > -INFINITY);
-    int len = make_list(!by_count, [&](float x) EE_ALWAYS_INLINE { return all ? x > -INFINITY : x >= from; });
+    // How many the list would have at least: counted, or from the masses, of which no token of
+    // bin b has more than e^(-b / 64).  (512 rows of 128000: top-p 0.95 231 us, trying first 239;
+    // top-k 20000 333, so 375.)
+    bool too_many = false;
+    if (bin < kBins - 1) {
+      double tokens = static_cast<double>(sh.before + sh.hist[bin]);
+      if (!by_count) {
+        float mine = 0.0f;
+#pragma unroll
+        for (int e = 0; e < PB; ++e)
+          if (tid * PB + e <= bin) mine += static_cast<float>(v[e]) * exp2f((tid * PB + e) * (1.0f / (kBinsPerUnit * static_cast<float>(kLn2))));
+        tokens = block_sum(static_cast<double>(mine)) / kUnit;
+      }
+      too_many = tokens > kList * 1.001;
+    }
+    int len = too_many ? kList + 1 : make_list(!by_count, [&](float x) EE_ALWAYS_INLINE { return all ? x > -INFINITY : x >= from; });
     if (len <= kSmallList) {
       if (wave == 0) {
         sort_wave(len);
@@ -857,8 +1051,8 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
   // then the same once more with that share divided among all waves, and that wave's ids one
   // by one.
   const double q = mass_of(value_of(tau)), tie_mass = q >= least ? q : 0.0;
-  // What the waves have is known from step 2 (slot 1, no ties), or from the list of the
-  // cut's bin, unless min-p takes some of it away again.
+  // What the waves (or the parts taken ahead) have is known from step 2 (slot 1, no ties), or
+  // from the list of the cut's bin, unless min-p takes some of it away again.
   const bool from_sums = !cut && least == 0.0, from_list = in_bin && least == 0.0;
   double before = 0.0, goal = 0.0, total = 0.0;
   int ties_before = 0, from = 0, width = chunk;
@@ -893,11 +1087,13 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
     // (step 2 left its sums, which have no ties, in slot 1)
     auto wave_of = [&](int w, int seen, int &t) EE_ALWAYS_INLINE {
       t = summed ? 0 : sh.ipart[0][w];
+      if (summed && splits > 0) return parts[w].z;
       return sh.part[summed ? 1 : 0][w] + min(max(ties - seen, 0), t) * tie_mass;
     };
     int t;
+    const int shares = summed && splits > 0 ? splits : W;
     if (level == 0) {
-      for (int w = 0, seen = 0; w < W; ++w) {
+      for (int w = 0, seen = 0; w < shares; ++w) {
         total += wave_of(w, seen, t);
         seen += t;
       }
@@ -905,7 +1101,7 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
     }
     int pick = -1;
     double upto = before;
-    for (int w = 0, seen = ties_before; w < W; ++w) {
+    for (int w = 0, seen = ties_before; w < shares; ++w) {
       const double mass = wave_of(w, seen, t);
       if (mass > 0.0 && (pick < 0 || upto <= goal)) {
         pick = w;
@@ -915,8 +1111,14 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
       upto += mass;
       seen += t;
     }
-    from = from + pick * width;
-    const int to = min(from + width, a.vocab);
+    int to;
+    if (summed && splits > 0) {
+      from = first_of_part(a.vocab, pick, splits);
+      to = min(first_of_part(a.vocab, pick + 1, splits), a.vocab);
+    } else {
+      from = from + pick * width;
+      to = min(from + width, a.vocab);
+    }
     if (level == 0) {
       width = share(from, to);
     } else {
@@ -976,24 +1178,51 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a) {
 // The largest row that LDS holds beside what else is there: 32000 fp32 logits.
 constexpr size_t kLds = 160 << 10;
 
-size_t sample_workspace(int, int) { return 256; }
+// Blocks a row that take the first two steps ahead, or 0, for rows that LDS does not hold: up
+// to 64 of them, one block of each with its own few waves reading, leave most of the card
+// idle.  A part is at least 16000 ids, as the sampling block adds up the parts' histograms.
+// 16 rows of 128000 fp32 logits, top-p 0.9: 62 us, in one block a row 96; 4 rows of 50021 40
+// and 56; 128 rows of 128000 are slower so, 111 and 105, and rows in LDS too (64 bf16 rows of
+// 50021: 53 and 47).
+int sample_splits(int n, int vocab) {
+  const int splits = std::min(256 / n, vocab / 16000);
+  return n <= 64 && splits >= 2 ? splits : 0;
+}
 
-hipError_t launch_sample(bool f32, const SampleArgs &a, void *, hipStream_t stream) {
+size_t sample_workspace(int n, int vocab) {
+  const size_t parts = static_cast<size_t>(n) * sample_splits(n, vocab);
+  return std::max<size_t>(256, (parts * sizeof(Part) + 255) / 256 * 256 + parts * kBins * 8);
+}
+
+hipError_t launch_sample(bool f32, const SampleArgs &a, void *ws, hipStream_t stream) {
   if (a.n <= 0) return hipSuccess;
   const size_t row = (static_cast<size_t>(a.vocab) + 3) / 4 * 4 * (f32 ? 4 : 2);
   const bool cached = shared_bytes(true) + row <= kLds;
   const size_t lds = shared_bytes(cached) + (cached ? row : 0);
+  const int splits = cached ? 0 : sample_splits(a.n, a.vocab);
+  Part *parts = static_cast<Part *>(ws);
+  auto *hists = reinterpret_cast<unsigned long long *>(
+      static_cast<char *>(ws) + (static_cast<size_t>(a.n) * splits * sizeof(Part) + 255) / 256 * 256);
   hipError_t e = hipSuccess;
   EE_DISPATCH(f32, {
+    if (splits > 0) {
+      const dim3 grid(splits, a.n), block(64 * kPartWaves);
+      hipLaunchKernelGGL(part_max_kernel<T>, grid, block, 0, stream, a, parts);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(part_sum_kernel<T>, grid, block, 0, stream, a, parts, hists);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
     auto go = [&](auto k, int waves) {
       e = hipFuncSetAttribute(reinterpret_cast<const void *>(k), hipFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(lds));
       if (e != hipSuccess) return;
-      hipLaunchKernelGGL(k, dim3(a.n), dim3(64 * waves), lds, stream, a);
+      hipLaunchKernelGGL(k, dim3(a.n), dim3(64 * waves), lds, stream, a, parts, hists, splits);
       e = hipGetLastError();
     };
     if (cached)
       go(sample_kernel<T, true, 16>, 16);
-    else if (a.n > 256)
+    else if (a.n > 256)  // two blocks of 8 waves a CU; 512 rows of 128000 fp32 logits, top-p 0.9: 201 us, in blocks of 16 217
       go(sample_kernel<T, false, 8>, 8);
     else
       go(sample_kernel<T, false, 16>, 16);

@@ -253,3 +253,36 @@ def test_equal_calls_and_replays_give_equal_results():
         go()
         torch.cuda.synchronize()
         assert torch.equal(a[0], token) and torch.equal(a[1], prob) and (token >= 0).all()
+
+
+@pytest.mark.parametrize("n,v,ld", [(1, 64001, 64001), (4, 256001, 256004), (64, 40961, 40962), (65, 40961, 40964)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["none", "top_p", "mixed"])
+def test_rows_that_several_blocks_read(n, v, ld, dtype, kind):
+    """Long rows, few of them: random numbers at both ends, a mask, and rows with no
+    distribution, by what lies in the first ids, in the middle and in the last ones."""
+    say(f"case: sample long {n}x{v} ld {ld} {dtype} {kind}")
+    g = np.random.default_rng(n + v)
+    x = torch.full((n, ld), float("nan"), device="cuda")
+    x[:, :v] = torch.from_numpy(logits(n, v, g)).cuda()
+    x = x.to(DTYPES[dtype][1])
+    u = g.random(n).astype(np.float32)
+    u[0] = np.nextafter(np.float32(1.0), np.float32(0.0))
+    u[n // 2] = 0.0
+    allowed = g.random((n, v)) < 0.7
+    allowed[:, v // 3] = True
+    how = params(n, g, kind)
+    check(x, u, run(x, u, ld=(v,), **how), vocab=v, **how)
+    check(x, u, run(x, u, allowed, ld=(v,), **how), allowed, vocab=v, **how)
+    if n < 3:
+        return
+    bad = x.clone()
+    bad[0, v - 1] = float("nan")
+    bad[1, 0] = float("inf")
+    bad[2, :v] = float("-inf")
+    allowed[3] = False
+    got = run(bad, u, allowed | (np.arange(n) < 3)[:, None], ld=(v,), **how)
+    for r in range(4):
+        assert [float(o[r]) for o in got] == [-1, 0, 0, 0], r
+    rest = {k: None if a is None else a[4:] for k, a in how.items()}
+    check(bad[4:], u[4:], [o[4:] for o in got], allowed[4:], vocab=v, **rest)
