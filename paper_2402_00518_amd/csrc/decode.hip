@@ -156,10 +156,12 @@ template <typename T> __device__ __forceinline__ void dstore4(T *p, f32x4_t v);
 template <> __device__ __forceinline__ void dstore4<float>(float *p, f32x4_t v) {
   *reinterpret_cast<f32x4_t *>(p) = v;
 }
+__device__ __forceinline__ u32x2_t dpack4(f32x4_t v) {
+  return u32x2_t{static_cast<uint32_t>(f32_to_bf16(v[0])) | (static_cast<uint32_t>(f32_to_bf16(v[1])) << 16),
+                 static_cast<uint32_t>(f32_to_bf16(v[2])) | (static_cast<uint32_t>(f32_to_bf16(v[3])) << 16)};
+}
 template <> __device__ __forceinline__ void dstore4<bf16_t>(bf16_t *p, f32x4_t v) {
-  const u32x2_t u = {static_cast<uint32_t>(f32_to_bf16(v[0])) | (static_cast<uint32_t>(f32_to_bf16(v[1])) << 16),
-                     static_cast<uint32_t>(f32_to_bf16(v[2])) | (static_cast<uint32_t>(f32_to_bf16(v[3])) << 16)};
-  *reinterpret_cast<u32x2_t *>(p) = u;
+  *reinterpret_cast<u32x2_t *>(p) = dpack4(v);
 }
 
 // f(row0, token, vals) for each group of 4 consecutive rows of the lane
@@ -284,57 +286,26 @@ struct DecLogits {
   }
 };
 
-// The logits themselves, out[j][ld] in fp32 or bf16; vec: groups of four of a row
-// are aligned.
+// The logits themselves, out[j][ld] in fp32 or bf16; rows need not be aligned (V 32003, 200
+// tokens, exit included: 75 us, whole rows through LDS 77).
 struct DecStoreLogits {
   static constexpr bool kSplit = false;
   struct Params {
     void *out;
     int64_t ld;
-    bool f32, vec;
+    bool f32;
   };
-  // Rows that are not aligned for wider stores: a wave's 64 vocabulary ids of NT tokens through
-  // its own LDS (256 bytes a token, 16-byte chunk c of token t at c ^ (t mod 16)), then 64
-  // consecutive logits of one token a store instead of pieces of 32 (V 32003, 200 tokens: 89
-  // -> 85 us).
-  template <int NT>
-  __device__ __forceinline__ static void apply_rows(const Params &p, const f32x16_t (&blk)[2][NT / 32], int r0, int j0,
-                                                    int lane, int R, int B, char *lds) {
-    static_for<2>([&](auto i) EE_ALWAYS_INLINE {
-      static_for<NT / 32>([&](auto j) EE_ALWAYS_INLINE {
-        constexpr int I = decltype(i)::value, J = decltype(j)::value;
-        static_for<4>([&](auto q) EE_ALWAYS_INLINE {
-          constexpr int Q = decltype(q)::value;
-          const int c = dec_row(32 * I, lane, 4 * Q) >> 2, t = 32 * J + (lane & 31);
-          *reinterpret_cast<f32x4_t *>(lds + t * 256 + ((c ^ (t & 15)) << 4)) =
-              f32x4_t{blk[I][J][4 * Q], blk[I][J][4 * Q + 1], blk[I][J][4 * Q + 2], blk[I][J][4 * Q + 3]};
-        });
-      });
-    });
-    wait_lgkm();
-    const int r = r0 + lane;
-    for (int t = 0; t < NT && j0 + t < B; ++t) {
-      const float v = *reinterpret_cast<const float *>(lds + t * 256 + (((lane >> 2) ^ (t & 15)) << 4) + (lane & 3) * 4);
-      const int64_t o = static_cast<int64_t>(j0 + t) * p.ld + r;
-      if (r < R) {
-        if (p.f32)
-          static_cast<float *>(p.out)[o] = v;
-        else
-          static_cast<bf16_t *>(p.out)[o] = f32_to_bf16(v);
-      }
-    }
-  }
   __device__ __forceinline__ static void apply(const Params &p, const f32x16_t &acc, int r0, int j0, int lane, int R,
                                                int B) {
     for_rows4(acc, r0, j0, lane, R, B, [&](int row0, int j, f32x4_t c) EE_ALWAYS_INLINE {
       const int64_t o = static_cast<int64_t>(j) * p.ld + row0;
       float *f = static_cast<float *>(p.out) + o;
       bf16_t *h = static_cast<bf16_t *>(p.out) + o;
-      if (p.vec && row0 + 4 <= R) {
+      if (row0 + 4 <= R) {
         if (p.f32)
-          dstore4<float>(f, c);
+          store_any(f, c);
         else
-          dstore4<bf16_t>(h, c);
+          store_any(h, dpack4(c));
         return;
       }
       static_for<4>([&](auto e) EE_ALWAYS_INLINE {
@@ -490,13 +461,6 @@ __global__ __launch_bounds__(BM / 64 * (BN / WN) * 64) void ring_kernel(Operand 
   f32x16_t blk[2][WN / 32];
   to_blocks32<2, WN / 32>(acc, blk);
   const int r0 = tile * BM + (wave / Rg::WAVES_N) * 64, t0 = j0 + (wave % Rg::WAVES_N) * WN;
-  if constexpr (std::is_same<Epi, DecStoreLogits>::value) {
-    static_assert(BM / 64 * (BN / WN) * WN * 256 <= NS * Rg::STAGE_BYTES, "room for every wave's logits");
-    if (!ep.vec) {  // (every wave has read the last stage, see Ring)
-      Epi::template apply_rows<WN>(ep, blk, r0, t0, lane, R, B, smem + wave * (WN * 256));
-      return;
-    }
-  }
   static_for<WN / 32>([&](auto j) EE_ALWAYS_INLINE {
     constexpr int J = decltype(j)::value;
     if constexpr (PAIR) {
@@ -723,7 +687,7 @@ hipError_t decode_logits(bool f32, const void *w_out, int vocab, const void *z, 
 
 hipError_t decode_store_logits(bool f32, const void *w_out, int vocab, const void *z, int n, int h, void *out, bool out_f32,
                                int64_t ld, hipStream_t stream) {
-  const DecStoreLogits::Params ep{out, ld, out_f32, ld % 4 == 0};
+  const DecStoreLogits::Params ep{out, ld, out_f32};
   if (f32 || decode_skinny_logits(vocab, n, h))
     EE_DISPATCH(f32, return (launch_skinny<T, DecStoreLogits>(w_out, h, vocab, z, h, n, h, ep, stream)));
   return launch_ring<DecStoreLogits, false>(Operand{w_out, h}, vocab, Operand{z, h}, n, h, 1, ep, stream);

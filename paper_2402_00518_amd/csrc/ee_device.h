@@ -17,6 +17,18 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 
+// A vector of memory that is aligned as its elements of type T only, in one access.
+template <typename V, typename T>
+__device__ __forceinline__ V load_any(const T *p) {
+  typedef V Any __attribute__((aligned(alignof(T))));
+  return *reinterpret_cast<const Any *>(p);
+}
+template <typename V, typename T>
+__device__ __forceinline__ void store_any(T *p, const V &v) {
+  typedef V Any __attribute__((aligned(alignof(T))));
+  *reinterpret_cast<Any *>(p) = v;
+}
+
 constexpr int kWave = 64;
 
 // Lambdas that touch register arrays must be inlined: an out-of-line call

@@ -173,7 +173,6 @@ struct Row {
   const uint32_t *allowed;
   Q *cache;
   int vocab, first, last;  // ids of the wave: [first, last)
-  bool vec;
   int lane;
   mutable bool stop = false;  // set by a pass's function: no further step
 
@@ -196,7 +195,7 @@ struct Row {
   }
   // Four ids from `id` < vocab on; past the vocabulary anything.
   __device__ __forceinline__ Q load(int id) const {
-    if (vec && id + 4 <= vocab) return *reinterpret_cast<const Q *>(p + id);
+    if (id + 4 <= vocab) return load_any<Q>(p + id);
     float x[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = to_f32(p[min(id + e, vocab - 1)]);
@@ -344,7 +343,6 @@ __device__ __forceinline__ Row<T, false> global_row(const SampleArgs &a, int n, 
   row.allowed = a.allowed != nullptr ? a.allowed + n * a.allowed_ld : nullptr;
   row.cache = nullptr;
   row.vocab = a.vocab;
-  row.vec = a.ld % 4 == 0;
   row.lane = lane;
   return row;
 }
@@ -454,7 +452,6 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a, const P
     return chunk;
   };
   const int chunk = share(0, a.vocab);
-  row.vec = a.ld % 4 == 0;
   row.lane = lane;
 
   int slot = 0;  // block sums alternate between two slots, one barrier each

@@ -137,7 +137,7 @@ struct StoreC {
   void *c;
   int64_t ld;
   int rows, features;
-  bool accumulate, vec, vec8;  // vec, vec8: groups of four (eight) features are aligned
+  bool accumulate;
 };
 
 __device__ __forceinline__ u32x2_t pack4(f32x4_t v) {
@@ -145,16 +145,16 @@ __device__ __forceinline__ u32x2_t pack4(f32x4_t v) {
                  static_cast<uint32_t>(f32_to_bf16(v[2])) | (static_cast<uint32_t>(f32_to_bf16(v[3])) << 16)};
 }
 
-// Four consecutive features of one row of C.
+// Four consecutive features of one row of C (whose rows need not be aligned).
 template <bool F32>
 __device__ __forceinline__ void store_c(const StoreC &s, int row, int f, f32x4_t v) {
   if (row >= s.rows || f >= s.features) return;
   const int64_t o = static_cast<int64_t>(row) * s.ld + f;
   if constexpr (F32) {
     float *p = static_cast<float *>(s.c) + o;
-    if (s.vec && f + 4 <= s.features) {
-      if (s.accumulate) v += *reinterpret_cast<const f32x4_t *>(p);
-      *reinterpret_cast<f32x4_t *>(p) = v;
+    if (f + 4 <= s.features) {
+      if (s.accumulate) v += load_any<f32x4_t>(p);
+      store_any(p, v);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -162,8 +162,8 @@ __device__ __forceinline__ void store_c(const StoreC &s, int row, int f, f32x4_t
     }
   } else {
     bf16_t *p = static_cast<bf16_t *>(s.c) + o;
-    if (s.vec && f + 4 <= s.features) {
-      *reinterpret_cast<u32x2_t *>(p) = pack4(v);
+    if (f + 4 <= s.features) {
+      store_any(p, pack4(v));
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -176,8 +176,8 @@ __device__ __forceinline__ void store_c(const StoreC &s, int row, int f, f32x4_t
 __device__ __forceinline__ void store_row8(const StoreC &s, int row, int f, u32x4_t v) {
   if (row >= s.rows || f >= s.features) return;
   bf16_t *p = static_cast<bf16_t *>(s.c) + static_cast<int64_t>(row) * s.ld + f;
-  if (s.vec8 && f + 8 <= s.features) {
-    *reinterpret_cast<u32x4_t *>(p) = v;
+  if (f + 8 <= s.features) {
+    store_any(p, v);
   } else {
     static_for<8>([&](auto e) EE_ALWAYS_INLINE {
       constexpr int E = decltype(e)::value;
@@ -194,6 +194,15 @@ __device__ __forceinline__ i32x8_t fragment(const bf16x8_t (&f)[2]) { return __b
 // wave's WM x WN outputs: a stage is KW blocks of K, one for each, and their sums meet in LDS.
 // ROW1: W's scales are one for each row, else one for each 128 (a wave's rows lie in one
 // block).  E5: Z's codes are e5m2.  WIDE: C is fp32.
+//
+// What bounds it, by K and tokens: the weights' trip from memory and the chain of load, barrier
+// and sum (5120 x 13824, 48 tokens: 28 us, 2.6 TB/s, 80 blocks), or, for an fp32 C of
+// thousands of tokens, the power that matrix and vector units draw together: 13824 x 5120, K
+// 4016, scales by rows: 605 to 650 us, 0.9 PFLOP/s, with the matrix units busy 37% and the
+// vector units 51% of the cycles (two instructions a product to widen, two to scale and add).
+// Products and vector work interleaved by hand with the next stage's first reads under the
+// last products took 656 us on the machine where this took 643, products of 32 x 32 outputs
+// 685, a third stage 657.
 template <int BM, int BN, int WM, int WN, int KW, int NS, bool ROW1, bool E5, bool WIDE>
 __global__ __launch_bounds__(BM / WM * (BN / WN) * KW * 64) void ring8_kernel(ScaledMat W, ScaledMat Z, int K, StoreC out) {
   constexpr int WAVES_N = BN / WN, WAVES = BM / WM * WAVES_N, THREADS = WAVES * KW * 64;
@@ -328,6 +337,8 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * KW * 64) void ring8_kernel(Sc
 // values.  A wave's 128 features are one block of the weight's scales, its lanes' tokens
 // have one scale each, so a stage needs four scale products a lane.  The scales of a stage
 // (256 features', 256 tokens') take one more load a thread, into one of four places in LDS.
+// 4096 tokens, 32000 x 4096: 470 to 490 us, 2.2 to 2.3 PFLOP/s, the matrix units busy 53% of
+// the cycles: 7.8 rounds of tiles, and the epilogue's 262 MB, which nothing hides.
 constexpr int kBigStages = 131072, kBigScales = 2048;
 
 template <bool E5>
@@ -506,7 +517,8 @@ __global__ __launch_bounds__(512, 1) void big8_kernel(ScaledMat W, ScaledMat Z, 
 
 // Few tokens, weights streamed once: a block has 16 RB features and up to 16 NB tokens, its
 // waves share K and read both operands straight into MFMA fragments, U blocks of K at a
-// time; their sums meet in LDS and each wave finishes some of the 16 x 16 blocks.
+// time; their sums meet in LDS and each wave finishes some of the 16 x 16 blocks.  The weights'
+// trip bounds it: 32000 x 4096, 1 token: 24 us, 5.5 TB/s (through an LDS ring 30 us).
 template <int RB, int NB, int WAVES, int U, bool ROW1, bool E5, bool WIDE>
 __global__ __launch_bounds__(64 * WAVES) void skinny8_kernel(ScaledMat W, ScaledMat Z, int K, StoreC out) {
   __shared__ f32x4_t red[WAVES][RB * NB][64];
@@ -696,7 +708,7 @@ hipError_t scaled_matmul(const ScaledMat &a, const ScaledMat &b, void *c, bool c
                          hipStream_t stream) {
   if (a.rows <= 0 || b.rows <= 0) return hipSuccess;
   if (((a.cols + 15) & ~15) != ((b.cols + 15) & ~15) || b.e5m2) return hipErrorInvalidValue;
-  const StoreC out{c, ldc, a.rows, b.rows, accumulate != 0, ldc % 4 == 0, ldc % 8 == 0};
+  const StoreC out{c, ldc, a.rows, b.rows, accumulate != 0};
   switch (scaled_tile(c_f32, b.shift == 0, b.rows, a.rows, b.cols)) {
     case kBig: {
       const dim3 grid(static_cast<unsigned>(cdiv(a.rows, 256)) * cdiv(b.rows, 256));
