@@ -328,7 +328,8 @@ ee_status ee_scaled_matmul(const ee_scaled *a, const ee_scaled *b, void *c, int3
  *   hidden   device [n_rows][h], dtype of the exit.
  *   logits   device [n_rows][ld], logits_dtype EE_F32 or EE_BF16, ld >= V; columns
  *            past V are left as they were.
- *   ws       device workspace of ws_bytes >= ee_logits_workspace_bytes(). */
+ *   ws       device workspace of ws_bytes >= ee_logits_workspace_bytes(), for one call
+ *            at a time; what it holds before and after does not matter. */
 size_t ee_logits_workspace_bytes(const ee_exit *e, const ee_scaled *w_out, int64_t n_rows);
 
 ee_status ee_exit_logits(const ee_exit *e, const ee_scaled *w_out, const void *hidden, int64_t n_rows, void *logits,
@@ -363,7 +364,8 @@ ee_status ee_exit_logits(const ee_exit *e, const ee_scaled *w_out, const void *h
  *   uniform  device [n_rows] fp32 in [0, 1).
  *   token    device [n_rows] int32;  prob, confidence (fp32) and exit_flag (int32)
  *            device [n_rows] or NULL.
- *   ws       device workspace of ws_bytes >= ee_sample_workspace_bytes(). */
+ *   ws       device workspace of ws_bytes >= ee_sample_workspace_bytes(), for one call at
+ *            a time; what it holds before and after does not matter. */
 typedef struct ee_sampling {
   const float *temperature;
   const int32_t *top_k;

@@ -265,6 +265,9 @@ struct RowPlan {
     top_p = a.top_p != nullptr ? a.top_p[n] : 1.0f;
     min_p = a.min_p != nullptr ? a.min_p[n] : 0.0f;
     u = a.uniform[n];
+  }
+  // (apart, as what is loaded is waited for here: before a row's own loads that took 0.8 us)
+  __device__ __forceinline__ void derive(const SampleArgs &a) {
     valid = temp == temp && top_p == top_p && min_p == min_p && u == u;
     greedy = !(temp > 0.0f);
     by_count = !greedy && top_k > 0 && top_k < a.vocab;
@@ -398,7 +401,8 @@ __global__ __launch_bounds__(64 * kPartWaves) void part_sum_kernel(SampleArgs a,
   __shared__ double sums[2][kPartWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.y;
   const int splits = gridDim.x, at = n * splits + blockIdx.x;
-  const RowPlan plan(a, n);
+  RowPlan plan(a, n);
+  plan.derive(a);
   bool bad = !plan.valid;
   const float mx = max_of_parts(parts + n * splits, splits, bad);
   if (bad || mx == INFINITY || mx == -INFINITY || !(plan.need_z || plan.need_z1 || plan.cut)) return;
@@ -431,14 +435,13 @@ __global__ __launch_bounds__(64 * kPartWaves) void part_sum_kernel(SampleArgs a,
 // W: waves of the block.  splits > 0: steps 1 and 2 have been taken by the kernels above.
 template <typename T, bool CACHED, int W>
 __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a, const Part *parts, const unsigned long long *hists,
-                                                           int splits) {
+                                                           int row_splits) {
+  const int splits = CACHED ? 0 : row_splits;
   constexpr int kThreads = 64 * W, kList = list_of(CACHED);
   extern __shared__ __attribute__((aligned(16))) char smem[];
   auto &sh = *reinterpret_cast<Shared<kList> *>(smem);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = blockIdx.x;
-  const RowPlan plan(a, n);
-  const int top_k = plan.top_k;
-  const float u = plan.u;
+  RowPlan plan(a, n);
   Row<T, CACHED> row;
   row.cache = reinterpret_cast<typename Quad<T>::type *>(smem + shared_bytes(CACHED));
   row.p = static_cast<const T *>(a.logits) + n * a.ld;
@@ -468,8 +471,9 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a, const P
 
   // 1. the maximum, and whether the row has a distribution at all
   float mx = -INFINITY;
-  bool bad = !plan.valid;
+  bool bad = false;
   if (splits > 0) {
+    plan.derive(a);
     parts += n * splits;
     hists += static_cast<int64_t>(n) * splits * kBins;
     mx = max_of_parts(parts, splits, bad);
@@ -494,8 +498,9 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a, const P
       }
     });
     mx = warp_max(mx);
-    bad = __any(bad);
+    plan.derive(a);
   }
+  bad = __any(bad) || !plan.valid;
   if (lane == 0) {
     sh.part[0][wave] = mx;
     sh.ipart[0][wave] = bad;
@@ -518,6 +523,8 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a, const P
     }
     return;
   }
+  const int top_k = plan.top_k;
+  const float u = plan.u;
   const bool by_count = plan.by_count, by_mass = plan.by_mass, cut = plan.cut;
   const double dmx = mx, least = plan.least, p = plan.p;
   const float bscale = plan.bscale;
