@@ -196,7 +196,7 @@ __device__ __forceinline__ i32x8_t fragment(const bf16x8_t (&f)[2]) { return __b
 // block).  E5: Z's codes are e5m2.  WIDE: C is fp32.
 //
 // What bounds it, by K and tokens: the weights' trip from memory and the chain of load, barrier
-// and sum (5120 x 13824, 48 tokens: 28 us, 2.6 TB/s, 80 blocks), or, for an fp32 C of
+// and sum (5120 x 13824, 48 tokens: 28 us, 2.6 TB/s, 160 blocks), or, for an fp32 C of
 // thousands of tokens, the power that matrix and vector units draw together: 13824 x 5120, K
 // 4016, scales by rows: 605 to 650 us, 0.9 PFLOP/s, with the matrix units busy 37% and the
 // vector units 51% of the cycles (two instructions a product to widen, two to scale and add).
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * KW * 64) void ring8_kernel(Sc
 // values.  A wave's 128 features are one block of the weight's scales, its lanes' tokens
 // have one scale each, so a stage needs four scale products a lane.  The scales of a stage
 // (256 features', 256 tokens') take one more load a thread, into one of four places in LDS.
-// 4096 tokens, 32000 x 4096: 470 to 490 us, 2.2 to 2.3 PFLOP/s, the matrix units busy 53% of
+// 4096 tokens, 32000 x 4096: 470 to 490 us, 2.2 to 2.3 PFLOP/s, the matrix units busy 54% of
 // the cycles: 7.8 rounds of tiles, and the epilogue's 262 MB, which nothing hides.
 constexpr int kBigStages = 131072, kBigScales = 2048;
 
