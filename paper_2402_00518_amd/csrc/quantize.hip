@@ -9,9 +9,9 @@
 //
 // Memory bounds it: every value is read once, held in registers as one 128 x 128 tile a
 // block (whose maxima need it whole, by rows, by columns or altogether) and its codes are
-// written once or, with the transpose, twice.  32000 x 4096 fp32 weights (655 MB): 117 us,
-// 5.6 TB/s; 4013 x 5120 bf16 with both outputs (82 MB): 22 us, 3.7 TB/s, 1280 tiles whose
-// reading, barriers, LDS turn and writing follow each other five tiles a CU; 8 rows of
+// written once or, with the transpose, twice.  32000 x 4096: fp32 weights (655 MB) 120 us,
+// bf16 73 us, 5.4 TB/s; 4001 x 5120 bf16 with both outputs (82 MB): 21 us, 3.9 TB/s, 1280 tiles
+// whose reading, barriers, LDS turn and writing follow each other, five tiles a CU; 8 rows of
 // 4096: 4 us, one launch.
 #include <hip/hip_runtime.h>
 
@@ -48,7 +48,7 @@ __device__ __forceinline__ float max16(float v) {  // over 16 consecutive lanes
 }
 
 // Eight values of a row from column c on (0 past the last column).  Rows need not be aligned
-// (4001 x 5124 bf16, both outputs: element by element 51 us, so 27).
+// (4001 x 5124 bf16, both outputs: element by element 51 us, so 24).
 template <typename T>
 __device__ __forceinline__ void load8(const T *row, int c, int cols, float (&v)[8]) {
   if (c + 8 <= cols) {
@@ -73,6 +73,36 @@ __device__ __forceinline__ void load8(const T *row, int c, int cols, float (&v)[
   for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? to_f32(row[c + e]) : 0.0f;
 }
 
+// Eight values as they are stored: bf16 ones in four registers, which leaves room for four
+// blocks a CU in place of three (32000 x 4096 bf16 100 -> 73 us).
+template <typename T>
+struct Eight {
+  float v[8];
+  __device__ __forceinline__ float operator[](int e) const { return v[e]; }
+  __device__ __forceinline__ void load(const float *row, int c, int cols) { load8(row, c, cols, v); }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+  }
+};
+template <>
+struct Eight<bf16_t> {
+  u32x4_t v;
+  __device__ __forceinline__ float operator[](int e) const {
+    return __uint_as_float(e % 2 == 0 ? v[e / 2] << 16 : v[e / 2] & 0xFFFF0000u);
+  }
+  __device__ __forceinline__ void load(const bf16_t *row, int c, int cols) {
+    if (c + 8 <= cols) {
+      v = load_any<u32x4_t>(row + c);
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      v[e] = (c + 2 * e < cols ? row[c + 2 * e] : 0u) | (c + 2 * e + 1 < cols ? static_cast<uint32_t>(row[c + 2 * e + 1]) << 16 : 0u);
+  }
+  __device__ __forceinline__ void clear() { v = u32x4_t{0, 0, 0, 0}; }
+};
+
 // One 128 x 128 tile a block of 256 threads: thread t holds columns 8 (t mod 16)
 // .. + 7 of rows 4 (t / 16) .. + 3 and those + 64.  Four consecutive rows a thread, so that
 // a column's codes pack into one 32-bit word on their way through LDS to the
@@ -90,15 +120,15 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T *__restrict__ x, 
   if (tr * 128 >= rows) return;
   const int c0 = tc * 128, r0 = tr * 128;
   const int c = (tid & 15) * 8, rg = tid >> 4;
-  float v[8][8], rowmax[8], cm[8];
+  Eight<T> v[8];
+  float rowmax[8], cm[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int r = r0 + rg * 4 + (i & 3) + (i >> 2) * 64;
     if (r < rows) {
-      load8(x + r * ldx, c0 + c, cols, v[i]);
+      v[i].load(x + r * ldx, c0 + c, cols);
     } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+      v[i].clear();
     }
   }
 #pragma unroll
@@ -308,8 +338,8 @@ hipError_t launch_quantize(bool f32, const void *x, int64_t ldx, int rows, int c
   const ScaledMat none{};
   const ScaledMat a = q != nullptr ? *q : none, b = qt != nullptr ? *qt : none;
   // Where a tile's pieces of rows end inside a cache line, the next tile along the row goes to the
-  // same XCD, whose L2 has the line: 32003 x 4095 bf16 119 us, in plain order 187; 9000 x
-  // 14000 fp32 123 and 151.  Else plain order spreads better: 32000 x 4096 bf16 88 us, so 97.
+  // same XCD, whose L2 has the line: 32003 x 4095 bf16 85 us, in plain order 154; 9000 x
+  // 14000 fp32 131 and 155.  Else plain order spreads better: 32000 x 4096 bf16 73 us, so 77.
   const bool apart = ldx * (f32 ? 4 : 2) % 128 != 0;
   const dim3 grid(((cols + 127) / 128 * ((rows + 127) / 128) + 7) / 8 * 8);
   EE_DISPATCH(f32, {
