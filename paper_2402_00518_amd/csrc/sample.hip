@@ -26,7 +26,7 @@
 //
 // What bounds it: not the bytes.  A row's block walks its ids two to five times with some 45
 // cycles of a SIMD for 64 exponentials and their histogram entries, and between the walks
-// stand scans, a sort and about thirty barriers: 18 to 24 us for one row of 32000, where
+// stand scans, a sort and about thirty barriers: 18 to 29 us for one row of 32000, where
 // reading it takes well under one.  512 rows of 128000 fp32 logits (262 MB, a pass over which
 // takes 46 us) with top-p 0.95: 231 us.
 #include <hip/hip_runtime.h>
@@ -384,14 +384,15 @@ __global__ __launch_bounds__(64 * kPartWaves) void part_max_kernel(SampleArgs a,
   }
 }
 
-// The row's maximum, and whether it has a NaN, from its parts.
-__device__ __forceinline__ float max_of_parts(const Part *parts, int splits, bool &bad) {
+// The row's maximum, and whether it has a NaN, from its parts (a part a lane).
+__device__ __forceinline__ float max_of_parts(const Part *parts, int splits, int lane, bool &bad) {
   float mx = -INFINITY;
-  for (int i = 0; i < splits; ++i) {
+  for (int i = lane; i < splits; i += 64) {
     mx = fmaxf(mx, parts[i].max);
     bad |= parts[i].bad != 0;
   }
-  return mx;
+  bad = __any(bad);
+  return warp_max(mx);
 }
 
 template <typename T>
@@ -404,7 +405,7 @@ __global__ __launch_bounds__(64 * kPartWaves) void part_sum_kernel(SampleArgs a,
   RowPlan plan(a, n);
   plan.derive(a);
   bool bad = !plan.valid;
-  const float mx = max_of_parts(parts + n * splits, splits, bad);
+  const float mx = max_of_parts(parts + n * splits, splits, lane, bad);
   if (bad || mx == INFINITY || mx == -INFINITY || !(plan.need_z || plan.need_z1 || plan.cut)) return;
   for (int i = tid; i < kBins; i += 64 * kPartWaves) hist[i] = 0;
   if (tid < 64) table[tid] = kPow2.v[tid];
@@ -476,12 +477,19 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a, const P
     plan.derive(a);
     parts += n * splits;
     hists += static_cast<int64_t>(n) * splits * kBins;
-    mx = max_of_parts(parts, splits, bad);
+    mx = max_of_parts(parts, splits, lane, bad);
     if (plan.cut) {
       for (int i = tid; i < kBins; i += kThreads) {
         unsigned long long h = 0;
-        if (!bad && mx < INFINITY && mx > -INFINITY)
-          for (int q = 0; q < splits; ++q) h += hists[static_cast<int64_t>(q) * kBins + i];
+        if (!bad && mx < INFINITY && mx > -INFINITY) {
+          for (int q = 0; q < splits; q += 8) {  // (eight loads in flight)
+            unsigned long long v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = q + e < splits ? hists[static_cast<int64_t>(q + e) * kBins + i] : 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h += v[e];
+          }
+        }
         sh.hist[i] = h;
       }
     }
@@ -535,10 +543,12 @@ __global__ __launch_bounds__(64 * W, 4) void sample_kernel(SampleArgs a, const P
   double z = 0.0, z1 = 0.0;
   if (splits > 0) {
     if (plan.need_z || plan.need_z1 || cut) {
-      for (int q = 0; q < splits; ++q) {
+      for (int q = lane; q < splits; q += 64) {
         z += parts[q].z;
         z1 += parts[q].z1;
       }
+      z = wave_sum(z);
+      z1 = wave_sum(z1);
     }
   } else if (plan.need_z || plan.need_z1 || cut) {
     sum_masses(row, plan, mx, sh.table, sh.hist, z, z1);
@@ -1185,8 +1195,8 @@ constexpr size_t kLds = 160 << 10;
 // Blocks a row that take the first two steps ahead, or 0, for rows that LDS does not hold: up
 // to 64 of them, one block of each with its own few waves reading, leave most of the card
 // idle.  A part is at least 16000 ids, as the sampling block adds up the parts' histograms.
-// 16 rows of 128000 fp32 logits, top-p 0.9: 62 us, in one block a row 96; 4 rows of 50021 40
-// and 56; 128 rows of 128000 are slower so, 111 and 105, and rows in LDS too (64 bf16 rows of
+// fp32 logits, top-p 0.9: 4 rows of 128000 56 us, in one block a row 93; 33 rows 61 and 99; 64
+// rows 80 and 101; 128 rows are slower so, 111 and 105, and rows in LDS too (64 bf16 rows of
 // 50021: 53 and 47).
 int sample_splits(int n, int vocab) {
   const int splits = std::min(256 / n, vocab / 16000);
